@@ -79,6 +79,7 @@ typedef int aqt_status;
 #define AQT_OP_LAYERNORM_BWD 16        /* M rows; K = row length; N unused                     */
 #define AQT_OP_MHSA_BWD 17             /* M = B * T tokens, K = model width D, N = heads       */
 #define AQT_OP_CONFORMER_LAYER_BWD 18  /* M = B * T tokens, K = model width D, N = inner width (heads <= 64, kernel <= 32 assumed) */
+#define AQT_OP_QK_NORM_ROTATE_BWD 19   /* M = B * T tokens, K = columns of a head; N unused    */
 
 /* What the forward keeps for the backward.  All caller-owned device buffers. */
 typedef struct aqt_saved {
@@ -607,6 +608,114 @@ aqt_status aqt_conformer_layer_bwd(const float *dy, const float *x, const aqt_co
                                    const aqt_conformer_layer_shape *shape, const aqt_layer_policy *policy,
                                    const aqt_conformer_layer_saved *saved, float *dx,
                                    const aqt_conformer_layer_grads *grads, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * Positions in the self-attention: queries and keys normalised per head and rotated by their
+ * frame's number, in one pass between the fused projection and the attention core (the paper
+ * leaves the encoding of positions open; aqt_attention_fwd by itself knows none).
+ * A row of qkv holds `heads` queries, `kv_heads` keys and `kv_heads` values of dh columns each
+ * ((heads + 2 kv_heads) dh columns; kv_heads == heads: the layout of aqt_attention_fwd).  For
+ * every query and key head x of frame number f = first[b] + t (first NULL: t):
+ *   n = x / sqrt(mean(x^2) + eps) * gamma     norm != 0; gamma_q / gamma_k nullable [dh] (ones)
+ *   (a, b) -> (a cos w - b sin w, a sin w + b cos w),  w = 2 pi f turns[i], for the pairs i < rot / 2
+ *             of its first rot columns: (i, i + rot / 2) or, AQT_ROTATE_PAIRS, (2 i, 2 i + 1)
+ * turns [rot / 2]: turns of a pair per frame, float64, e.g. from aqt_rotation_turns; the angle is
+ * taken in float64 and reduced there, so frames may be numbered far.  rot = 0: no rotation.
+ */
+#define AQT_ROTATE_HALVES 0
+#define AQT_ROTATE_PAIRS 1
+typedef struct aqt_qk_norm_rotate {
+  int heads, kv_heads, dh;   /* kv_heads divides heads; dh <= 128               */
+  int norm;                  /* 0: rotation only                                */
+  float eps;                 /* >= 0                                            */
+  int rot, pairing;          /* even, 0 .. dh; AQT_ROTATE_*                     */
+  const float *gamma_q;      /* nullable [dh]                                   */
+  const float *gamma_k;      /* nullable [dh]                                   */
+  const double *turns;       /* [rot / 2]; may be NULL when rot is 0            */
+} aqt_qk_norm_rotate;
+
+/* turns[i] = base^(-2 i / rot) / (2 pi), i < rot / 2 (rot <= 128, base > 0): the usual geometric series. */
+aqt_status aqt_rotation_turns(int rot, double base, double *turns, void *stream);
+
+/*
+ * out [B*T, (heads + 2 kv_heads) dh]: rotated queries and keys, values as they are.  out may be
+ * qkv itself (the values are then not touched), but not overlap it otherwise.
+ */
+aqt_status aqt_qk_norm_rotate_fwd(const float *qkv, int64_t B, int64_t T, const aqt_qk_norm_rotate *spec,
+                                  const int64_t *first, float *out, void *stream);
+
+/*
+ * Its gradient: dqkv from dout (the gradient with respect to out), with qkv the input of the
+ * forward (only read for norm; NULL is accepted without).  dqkv may be dout itself.
+ * dgamma_q / dgamma_k nullable [dh]: summed over rows and heads in a fixed order, only with norm;
+ * they need aqt_workspace_bytes(AQT_OP_QK_NORM_ROTATE_BWD, B*T, dh, ., ., .) of workspace.
+ */
+aqt_status aqt_qk_norm_rotate_bwd(const float *qkv, const float *dout, int64_t B, int64_t T,
+                                  const aqt_qk_norm_rotate *spec, const int64_t *first, float *dqkv,
+                                  float *dgamma_q, float *dgamma_k, void *ws, size_t ws_bytes, void *stream);
+
+/*
+ * Quantized cache of keys and values for streaming (Sec. 3.3: causal layers with limited left
+ * context): every stream keeps its last `capacity` frames as codes, one scale per frame and head
+ * for the key and one for the value, symmetric abs-max over the head as in Fig. 2.  bits 2..8;
+ * up to 4 the codes are two to a byte.
+ *   length [streams]: frames that each stream has behind it, in front of the call.  The calls below
+ *   take their new frames from there on and do not move it, so that the caches of all layers share
+ *   one array; aqt_cache_advance moves it when the step is over.  A negative length counts as 0.
+ *   count, nullable [streams]: how many of the T frames of the call each stream really brings (the
+ *   first ones; NULL: all; values outside 0..T count as the nearest).  What belongs to the other
+ *   rows is neither read nor written.
+ * Lengths and counts live on the device: nothing in these calls waits for them, and a captured
+ * step follows them from replay to replay.  The buffer needs no clearing.
+ */
+typedef struct aqt_cache {
+  int64_t streams;
+  int64_t capacity;          /* frames per stream, a multiple of 64                         */
+  int kv_heads, dh, bits;    /* dh <= 128                                                   */
+  void *data;                /* aqt_cache_bytes() bytes, 16-byte aligned                    */
+  const int64_t *length;     /* [streams]                                                   */
+} aqt_cache;
+
+/* Bytes of the buffer (host computation, data and length are not looked at); 0 on bad arguments. */
+size_t aqt_cache_bytes(const aqt_cache *shape);
+
+/*
+ * Write the keys and values of T new frames per stream, qkv [streams * T, (heads + 2 kv_heads) dh]
+ * (rows as above), into the cache: stream b's frame length[b] + t takes the place of the one
+ * `capacity` frames before it (of a call longer than the capacity only the last frames stay).
+ * *dev_status is set to AQT_ERR_NONFINITE when a head's abs-max is Inf/NaN.
+ */
+aqt_status aqt_cache_append(const float *qkv, int64_t T, int heads, const aqt_cache *cache, const int32_t *count,
+                            void *stream, int32_t *dev_status);
+
+/*
+ * Read n frames per stream back as code * scale: keys and / or values (either may be NULL)
+ * [streams * n, kv_heads dh], row (b, i) from frame first[b] + i; first NULL: the last n.
+ * The stream has length[b] + (count ? count[b] : pending) frames then: pending / count name what was
+ * appended and not advanced over yet (pending >= 0; 0 with count NULL: the length as it stands).
+ * Frames that it does not have, or the cache no longer holds, read as zeros.
+ */
+aqt_status aqt_cache_read(const aqt_cache *cache, int64_t pending, const int32_t *count, const int64_t *first,
+                          int64_t n, float *keys, float *values, void *stream);
+
+/* length[b] += count[b] (NULL: T; a negative length counts as 0), after the last layer's calls of a step. */
+aqt_status aqt_cache_advance(int64_t *length, int64_t streams, int64_t T, const int32_t *count, void *stream);
+
+/*
+ * aqt_attention_fwd over the cache: the queries of the T new frames (already appended) over the
+ * frames j that the cache holds with f - left_context <= j <= f + right_context, f = length[b] + t
+ * (a negative limit: none on that side; nothing lies behind the stream's last new frame).
+ * qkv as in aqt_cache_append, only the query columns are read; query heads h of a group of
+ * heads / kv_heads share key / value head h / (heads / kv_heads).  ctx [streams * T, heads dh]: rows
+ * of frames that a stream does not bring stay as they are; a row that sees no frame (its window lies
+ * before what the cache still holds) is zeros.  ctx_absmax nullable device float: max|ctx| over the
+ * written rows, cleared by the call.  A non-finite query gives NaN in its row.
+ * Needs aqt_attention_cached_workspace_bytes() (it does not depend on lengths or windows).
+ */
+size_t aqt_attention_cached_workspace_bytes(const aqt_cache *cache, int64_t T, int heads);
+aqt_status aqt_attention_cached_fwd(const float *qkv, int64_t T, int heads, const aqt_cache *cache, const int32_t *count,
+                                    int left_context, int right_context, float *ctx, float *ctx_absmax, void *ws,
+                                    size_t ws_bytes, void *stream);
 
 #ifdef __cplusplus
 }

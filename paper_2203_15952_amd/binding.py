@@ -23,8 +23,9 @@ AQT_EPI_NONE, AQT_EPI_SWISH, AQT_EPI_GLU = 0, 1, 2
  AQT_OP_DENSE_FWD_WONLY, AQT_OP_DENSE_BWD_EPI, AQT_OP_LAYERNORM_QUANTIZE, AQT_OP_FFN_FWD, AQT_OP_FFN_BWD,
  AQT_OP_DEPTHWISE_CONV_BWD, AQT_OP_CONV_MODULE_FWD, AQT_OP_CONV_MODULE_BWD, AQT_OP_MHSA_FWD,
  AQT_OP_CONFORMER_LAYER_FWD, AQT_OP_ATTENTION_BWD, AQT_OP_LAYERNORM_BWD, AQT_OP_MHSA_BWD,
- AQT_OP_CONFORMER_LAYER_BWD) = range(19)
+ AQT_OP_CONFORMER_LAYER_BWD, AQT_OP_QK_NORM_ROTATE_BWD) = range(20)
 AQT_POLICY_ALL, AQT_POLICY_EXCEPT_FIRST_LAST, AQT_POLICY_EXCEPT_ATTENTION, AQT_POLICY_FIRST_K = range(4)
+AQT_ROTATE_HALVES, AQT_ROTATE_PAIRS = 0, 1
 
 # every symbol include/aqt.h declares
 SYMBOLS = ["aqt_status_string", "aqt_last_hip_error", "aqt_version", "aqt_workspace_bytes",
@@ -36,7 +37,9 @@ SYMBOLS = ["aqt_status_string", "aqt_last_hip_error", "aqt_version", "aqt_worksp
            "aqt_prepare_weights", "aqt_dense_fwd_q_prepared", "aqt_depthwise_conv_fwd", "aqt_depthwise_conv_bwd",
            "aqt_conv_module_fwd", "aqt_conv_module_bwd", "aqt_attention_fwd", "aqt_mhsa_fwd",
            "aqt_residual_add", "aqt_conformer_layer_fwd", "aqt_attention_bwd",
-           "aqt_layernorm_bwd", "aqt_mhsa_bwd", "aqt_conformer_layer_bwd"]
+           "aqt_layernorm_bwd", "aqt_mhsa_bwd", "aqt_conformer_layer_bwd",
+           "aqt_rotation_turns", "aqt_qk_norm_rotate_fwd", "aqt_qk_norm_rotate_bwd", "aqt_cache_bytes", "aqt_cache_append",
+           "aqt_cache_read", "aqt_cache_advance", "aqt_attention_cached_workspace_bytes", "aqt_attention_cached_fwd"]
 
 
 class AqtError(RuntimeError):
@@ -103,6 +106,17 @@ class aqt_conformer_layer_saved(ctypes.Structure):
 
 class aqt_conformer_layer_grads(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in LAYER_WEIGHT_NAMES]
+
+
+class aqt_qk_norm_rotate(ctypes.Structure):
+    _fields_ = [("heads", ctypes.c_int), ("kv_heads", ctypes.c_int), ("dh", ctypes.c_int), ("norm", ctypes.c_int),
+                ("eps", ctypes.c_float), ("rot", ctypes.c_int), ("pairing", ctypes.c_int), ("gamma_q", ctypes.c_void_p),
+                ("gamma_k", ctypes.c_void_p), ("turns", ctypes.c_void_p)]
+
+
+class aqt_cache(ctypes.Structure):
+    _fields_ = [("streams", ctypes.c_int64), ("capacity", ctypes.c_int64), ("kv_heads", ctypes.c_int), ("dh", ctypes.c_int),
+                ("bits", ctypes.c_int), ("data", ctypes.c_void_p), ("length", ctypes.c_void_p)]
 
 
 _lib = None
@@ -184,6 +198,18 @@ def lib() -> ctypes.CDLL:
                                               ctypes.POINTER(aqt_layer_policy),
                                               ctypes.POINTER(aqt_conformer_layer_saved), _vp,
                                               ctypes.POINTER(aqt_conformer_layer_grads), _vp, _sz, _vp]
+        spec, cache = ctypes.POINTER(aqt_qk_norm_rotate), ctypes.POINTER(aqt_cache)
+        L.aqt_rotation_turns.argtypes = [_int, ctypes.c_double, _vp, _vp]
+        L.aqt_qk_norm_rotate_fwd.argtypes = [_vp, _i64, _i64, spec, _vp, _vp, _vp]
+        L.aqt_qk_norm_rotate_bwd.argtypes = [_vp, _vp, _i64, _i64, spec, _vp, _vp, _vp, _vp, _vp, _sz, _vp]
+        L.aqt_cache_bytes.restype = _sz
+        L.aqt_cache_bytes.argtypes = [cache]
+        L.aqt_cache_append.argtypes = [_vp, _i64, _int, cache, _vp, _vp, _vp]
+        L.aqt_cache_read.argtypes = [cache, _i64, _vp, _vp, _i64, _vp, _vp, _vp]
+        L.aqt_cache_advance.argtypes = [_vp, _i64, _i64, _vp, _vp]
+        L.aqt_attention_cached_workspace_bytes.restype = _sz
+        L.aqt_attention_cached_workspace_bytes.argtypes = [cache, _i64, _int]
+        L.aqt_attention_cached_fwd.argtypes = [_vp, _i64, _int, cache, _vp, _int, _int, _vp, _vp, _vp, _sz, _vp]
         for name in SYMBOLS:
             getattr(L, name)  # AttributeError if the library lacks a declared entry point
         _lib = L
@@ -851,3 +877,153 @@ def aqt_conformer_layer_bwd(dy, x, weights: dict, saved: LayerSaved, *, B: int, 
                                        _ptr(ws), ws.numel(), _stream())
     _check(st, "aqt_conformer_layer_bwd")
     return dx, grads
+
+
+def _shaped(t: Optional[torch.Tensor], dtype, shape, device, name: str):
+    """A contiguous device tensor of exactly that type and shape, on the device the call runs on (None passes)."""
+    if t is not None and not (t.dtype == dtype and tuple(t.shape) == tuple(shape) and t.is_contiguous() and t.device == device):
+        raise TypeError(f"{name}: expected a contiguous {dtype} tensor {tuple(shape)} on {device}")
+    return t
+
+
+def _current(t: torch.Tensor, name: str):
+    """The launches go to the current device's current stream."""
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name}: expected a tensor on the current device")
+    return t.device
+
+
+class QkNormRotate:
+    """How queries and keys of rows with `heads` queries, `kv_heads` keys and values of dh columns are normalised and rotated
+    (aqt_qk_norm_rotate_fwd / _bwd), and its aqt_qk_norm_rotate view.  rot: leading columns of a head that are rotated (default:
+    all that make pairs); base: of the geometric series of angles, or turns, float64 [rot / 2] turns per frame, in its place.
+    gamma_q / gamma_k: float32 [dh] on the device, kept by reference (an optimizer may change them in place)."""
+
+    def __init__(self, heads: int, kv_heads: int, dh: int, *, rot: Optional[int] = None, base: float = 10000.0, turns=None,
+                 pairing: int = AQT_ROTATE_HALVES, norm: bool = True, eps: float = 1e-6, gamma_q=None, gamma_k=None, device="cuda"):
+        self.heads, self.kv_heads, self.dh, self.norm = heads, kv_heads, dh, bool(norm)
+        rot = dh // 2 * 2 if rot is None else rot
+        self.columns = (heads + 2 * kv_heads) * dh
+        self.gamma_q, self.gamma_k = gamma_q, gamma_k
+        for name, t in (("gamma_q", gamma_q), ("gamma_k", gamma_k)):
+            if t is not None:
+                _shaped(_dev(t, torch.float32, name), torch.float32, (dh,), t.device, name)
+        if turns is not None:
+            _shaped(_dev(turns, torch.float64, "turns"), torch.float64, (rot // 2,), turns.device, "turns")
+        elif rot:
+            turns = torch.empty(max(rot // 2, 1), dtype=torch.float64, device=device)
+            _check(lib().aqt_rotation_turns(rot, base, _ptr(turns), _stream()), "aqt_rotation_turns")
+        self.turns = turns
+        self.c = aqt_qk_norm_rotate(heads, kv_heads, dh, int(self.norm), eps, rot, pairing,
+                                    None if gamma_q is None else gamma_q.data_ptr(), None if gamma_k is None else gamma_k.data_ptr(),
+                                    None if turns is None else turns.data_ptr())
+
+
+def aqt_qk_norm_rotate_fwd(qkv, B: int, T: int, spec: QkNormRotate, *, first=None, out=None):
+    """aqt_qk_norm_rotate_fwd: qkv [B*T, (heads + 2 kv_heads) dh] -> out of the same shape (out=qkv: in place).
+    first: int64 [B], the frame number of every utterance's first row (default 0)."""
+    dev = _current(qkv, "qkv")
+    _shaped(qkv, torch.float32, (B * T, spec.columns), dev, "qkv")
+    _shaped(first, torch.int64, (B,), dev, "first")
+    out = torch.empty_like(qkv) if out is None else _shaped(out, torch.float32, qkv.shape, dev, "out")
+    _check(lib().aqt_qk_norm_rotate_fwd(qkv.data_ptr(), B, T, ctypes.byref(spec.c), None if first is None else first.data_ptr(),
+                                        out.data_ptr(), _stream()), "aqt_qk_norm_rotate_fwd")
+    return out
+
+
+def aqt_qk_norm_rotate_bwd(qkv, dout, B: int, T: int, spec: QkNormRotate, *, first=None, dqkv=None, want_gamma=True, ws=None):
+    """aqt_qk_norm_rotate_bwd: returns (dqkv, dgamma_q [dh] or None, dgamma_k [dh] or None); qkv is the forward's input
+    (dqkv=dout: in place).  The gradients of the gains come with norm only."""
+    dev = _current(dout, "dout")
+    _shaped(dout, torch.float32, (B * T, spec.columns), dev, "dout")
+    _shaped(qkv, torch.float32, dout.shape, dev, "qkv")
+    _shaped(first, torch.int64, (B,), dev, "first")
+    dqkv = torch.empty_like(dout) if dqkv is None else _shaped(dqkv, torch.float32, dout.shape, dev, "dqkv")
+    dq = dk = None
+    if want_gamma and spec.norm:
+        dq, dk = (torch.empty(spec.dh, dtype=torch.float32, device=dev) for _ in range(2))
+        ws = workspace(aqt_workspace_bytes(AQT_OP_QK_NORM_ROTATE_BWD, B * T, spec.dh, 1), dev) if ws is None else ws
+    _check(lib().aqt_qk_norm_rotate_bwd(None if qkv is None else qkv.data_ptr(), dout.data_ptr(), B, T, ctypes.byref(spec.c),
+                                        None if first is None else first.data_ptr(), dqkv.data_ptr(), _ptr(dq), _ptr(dk), _ptr(ws),
+                                        0 if ws is None else ws.numel(), _stream()), "aqt_qk_norm_rotate_bwd")
+    return dqkv, dq, dk
+
+
+class KvCache:
+    """A quantized cache of keys and values (aqt_cache_append, aqt_cache_read, aqt_attention_cached_fwd): its buffer, the streams'
+    lengths (int64 [streams], zeros unless given: the caches of all layers of a model share one) and its aqt_cache view."""
+
+    def __init__(self, streams: int, capacity: int, kv_heads: int, dh: int, bits: int = 8, *, length=None, device="cuda"):
+        self.streams, self.capacity, self.kv_heads, self.dh, self.bits = streams, capacity, kv_heads, dh, bits
+        self.c = aqt_cache(streams, capacity, kv_heads, dh, bits, None, None)
+        nbytes = int(lib().aqt_cache_bytes(ctypes.byref(self.c)))
+        if nbytes == 0:
+            raise AqtError(AQT_ERR_INVALID_ARG, "aqt_cache_bytes")
+        self.data = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        self.length = torch.zeros(streams, dtype=torch.int64, device=device) if length is None else length
+        _shaped(self.length, torch.int64, (streams,), self.data.device, "length")
+        self.c.data, self.c.length = self.data.data_ptr(), self.length.data_ptr()
+
+    def advance(self, T: int, count=None):
+        """aqt_cache_advance: the streams have T (or count[b]) frames more; after the last layer of a step."""
+        dev = _current(self.length, "length")
+        _shaped(count, torch.int32, (self.streams,), dev, "count")
+        _check(lib().aqt_cache_advance(_ptr(self.length), self.streams, T, _ptr(count), _stream()), "aqt_cache_advance")
+        return self
+
+
+def _new_rows(qkv, cache: KvCache, T: int, heads: int, count):
+    dev = _current(qkv, "qkv")
+    _shaped(qkv, torch.float32, (cache.streams * T, (heads + 2 * cache.kv_heads) * cache.dh), dev, "qkv")
+    _shaped(count, torch.int32, (cache.streams,), dev, "count")
+    if cache.data.device != dev:
+        raise ValueError("cache: expected a cache on the current device")
+    return dev
+
+
+def aqt_cache_append(qkv, cache: KvCache, T: int, heads: int, *, count=None, dev_status=None):
+    """aqt_cache_append: quantize the keys and values of qkv [streams*T, (heads + 2 kv_heads) dh] into the cache, behind the
+    frames that cache.length names.  count: int32 [streams], how many of the T frames each stream brings."""
+    _new_rows(qkv, cache, T, heads, count)
+    _check(lib().aqt_cache_append(qkv.data_ptr(), T, heads, ctypes.byref(cache.c), None if count is None else count.data_ptr(), _stream(),
+                                  None if dev_status is None else dev_status.data_ptr()), "aqt_cache_append")
+
+
+def aqt_cache_read(cache: KvCache, n: int, *, first=None, pending: int = 0, count=None, keys=None, values=None, want_keys=True,
+                   want_values=True):
+    """aqt_cache_read: returns (keys, values) float32 [streams*n, kv_heads dh], the frames first[b] .. (int64 [streams]; default
+    the last n).  pending / count: appended frames that cache.length does not count yet."""
+    dev = _current(cache.data, "cache")
+    shape = (cache.streams * n, cache.kv_heads * cache.dh)
+    _shaped(first, torch.int64, (cache.streams,), dev, "first")
+    _shaped(count, torch.int32, (cache.streams,), dev, "count")
+    if want_keys:
+        keys = torch.empty(shape, dtype=torch.float32, device=dev) if keys is None else _shaped(keys, torch.float32, shape, dev, "keys")
+    if want_values:
+        values = torch.empty(shape, dtype=torch.float32, device=dev) if values is None else _shaped(values, torch.float32, shape, dev, "values")
+    keys, values = keys if want_keys else None, values if want_values else None
+    _check(lib().aqt_cache_read(ctypes.byref(cache.c), pending, None if count is None else count.data_ptr(),
+                                None if first is None else first.data_ptr(), n, _ptr(keys), _ptr(values), _stream()), "aqt_cache_read")
+    return keys, values
+
+
+def aqt_attention_cached_workspace_bytes(cache: KvCache, T: int, heads: int) -> int:
+    return int(lib().aqt_attention_cached_workspace_bytes(ctypes.byref(cache.c), T, heads))
+
+
+def aqt_attention_cached_fwd(qkv, cache: KvCache, T: int, heads: int, *, left: int = -1, right: int = 0, count=None, ctx=None,
+                             want_absmax=False, ws=None):
+    """aqt_attention_cached_fwd: attention of the T new frames of every stream (appended before) over the cache; returns
+    (ctx [streams*T, heads dh], absmax word or None).  With count and no ctx given, the rows of other frames are zeros."""
+    dev = _new_rows(qkv, cache, T, heads, count)
+    shape = (cache.streams * T, heads * cache.dh)
+    if ctx is None:
+        ctx = (torch.empty if count is None else torch.zeros)(shape, dtype=torch.float32, device=dev)
+    else:
+        _shaped(ctx, torch.float32, shape, dev, "ctx")
+    m = torch.empty(1, dtype=torch.float32, device=dev) if want_absmax else None
+    ws = workspace(aqt_attention_cached_workspace_bytes(cache, T, heads), dev) if ws is None else ws
+    _check(lib().aqt_attention_cached_fwd(qkv.data_ptr(), T, heads, ctypes.byref(cache.c), None if count is None else count.data_ptr(),
+                                          left, right, ctx.data_ptr(), None if m is None else m.data_ptr(), ws.data_ptr(), ws.numel(),
+                                          _stream()), "aqt_attention_cached_fwd")
+    return ctx, m

@@ -1,6 +1,7 @@
 // C ABI of libaqt: argument checks, workspace carving and dispatch.  Every entry
 // point is declared and documented in include/aqt.h.
 #include "aqt_internal.h"
+#include "cache.h"
 
 namespace aqt {
 thread_local int g_last_hip_error = 0;
@@ -499,6 +500,36 @@ static aqt_status mhsa_bwd_check(const float *dy, const aqt_mhsa_saved *saved, i
   return AQT_OK;
 }
 
+namespace {
+// ---- checks of the entry points around positions and the cache ----
+size_t rotate_row_bytes(const aqt_qk_norm_rotate &s) {
+  return (static_cast<size_t>(s.heads) + 2 * static_cast<size_t>(s.kv_heads)) * s.dh * sizeof(float);
+}
+
+aqt_status rotate_check(int64_t B, int64_t T, const aqt_qk_norm_rotate *s) {
+  if (!s || B < 1 || T < 1 || s->heads < 1 || s->kv_heads < 1 || s->heads % s->kv_heads || s->dh < 1) return AQT_ERR_INVALID_ARG;
+  if (s->rot < 0 || s->rot % 2 || s->rot > s->dh || (s->rot && !s->turns) || !(s->eps >= 0.0f)) return AQT_ERR_INVALID_ARG;
+  if (s->pairing != AQT_ROTATE_HALVES && s->pairing != AQT_ROTATE_PAIRS) return AQT_ERR_INVALID_ARG;
+  if (s->dh > 128 || s->heads > (1 << 20)) return AQT_ERR_UNSUPPORTED;
+  return T <= (int64_t(1) << 50) / B ? AQT_OK : AQT_ERR_UNSUPPORTED;   // (2^50 rows: the rest is the tensor's own limit)
+}
+
+aqt_status cache_check(const aqt_cache *c) {
+  if (!c || c->streams < 1 || c->capacity < 1 || c->capacity % 64 || c->kv_heads < 1 || c->dh < 1) return AQT_ERR_INVALID_ARG;
+  return cache_shape_ok(*c) ? AQT_OK : AQT_ERR_UNSUPPORTED;
+}
+
+bool cache_buffers_ok(const aqt_cache &c) {
+  return c.data && c.length && reinterpret_cast<uintptr_t>(c.data) % 16 == 0;
+}
+
+aqt_status cache_call_check(const aqt_cache *c, int64_t T, int heads) {
+  if (!cache_buffers_ok(*c) || T < 1 || heads < 1 || heads % c->kv_heads) return AQT_ERR_INVALID_ARG;
+  return heads <= (1 << 20) && T <= (int64_t(1) << 40) ? AQT_OK : AQT_ERR_UNSUPPORTED;
+}
+
+}  // namespace
+
 extern "C" {
 
 const char *aqt_status_string(aqt_status s) {
@@ -569,6 +600,9 @@ size_t aqt_workspace_bytes(int op, int64_t M, int64_t K, int64_t N, int bits_x, 
     case AQT_OP_CONFORMER_LAYER_BWD:
       if (!shape_ok(M, K) || N < 1) return 0;
       return carve_layer_bwd(nullptr, M, K, N, 64, 32).total;
+    case AQT_OP_QK_NORM_ROTATE_BWD:
+      if (M < 1 || K < 1 || K > 128) return 0;
+      return rotate_bwd_ws_bytes(static_cast<int>(K));
     case AQT_OP_CONV_MODULE_BWD:
       if (!shape_ok(M, K) || N < 1 || N > 4096) return 0;
       return carve_conv_bwd(nullptr, 1, M, K, static_cast<int>(N)).total;
@@ -1068,6 +1102,82 @@ aqt_status aqt_conformer_layer_bwd(const float *dy, const float *x, const aqt_co
                       grads->ffn1_b2, ws, f.module, stream));
   AQT_TRY(ln_bwd(4, x, saved->ffn1.row_stats, w->ffn1_ln_g, f.dm, f.db, dx, grads->ffn1_ln_g, grads->ffn1_ln_b, nullptr));
   return launch_ln_folds(folds, defer ? kLnFoldsMax : 0, g.D, st);
+}
+
+// ---- positions and the quantized cache of the self-attention ---------------------------------
+
+aqt_status aqt_rotation_turns(int rot, double base, double *turns, void *stream) {
+  if (!turns || rot < 2 || rot % 2 || !(base > 0.0) || base > 1e300) return AQT_ERR_INVALID_ARG;
+  if (rot > 128) return AQT_ERR_UNSUPPORTED;
+  return launch_rotation_turns(rot, base, turns, static_cast<hipStream_t>(stream));
+}
+
+aqt_status aqt_qk_norm_rotate_fwd(const float *qkv, int64_t B, int64_t T, const aqt_qk_norm_rotate *spec, const int64_t *first,
+                                  float *out, void *stream) {
+  AQT_TRY(rotate_check(B, T, spec));
+  if (!qkv || !out) return AQT_ERR_INVALID_ARG;
+  const size_t bytes = rotate_row_bytes(*spec) * B * T;
+  if (out != qkv && overlap(qkv, bytes, out, bytes)) return AQT_ERR_INVALID_ARG;
+  return launch_rotate_fwd(qkv, B, T, *spec, first, out, static_cast<hipStream_t>(stream));
+}
+
+aqt_status aqt_qk_norm_rotate_bwd(const float *qkv, const float *dout, int64_t B, int64_t T, const aqt_qk_norm_rotate *spec,
+                                  const int64_t *first, float *dqkv, float *dgamma_q, float *dgamma_k, void *ws, size_t ws_bytes,
+                                  void *stream) {
+  AQT_TRY(rotate_check(B, T, spec));
+  const bool gains = dgamma_q || dgamma_k;
+  if (!dout || !dqkv || (spec->norm && !qkv) || (gains && !spec->norm)) return AQT_ERR_INVALID_ARG;
+  const size_t bytes = rotate_row_bytes(*spec) * B * T;
+  if ((dqkv != dout && overlap(dout, bytes, dqkv, bytes)) || overlap(qkv, spec->norm ? bytes : 0, dqkv, bytes)) return AQT_ERR_INVALID_ARG;
+  if (gains && (!ws || ws_bytes < rotate_bwd_ws_bytes(spec->dh))) return AQT_ERR_WORKSPACE;
+  return launch_rotate_bwd(qkv, dout, B, T, *spec, first, dqkv, dgamma_q, dgamma_k, ws, static_cast<hipStream_t>(stream));
+}
+
+size_t aqt_cache_bytes(const aqt_cache *shape) {
+  if (cache_check(shape) != AQT_OK) return 0;
+  const CacheGeom g = cache_geom(*shape);
+  return static_cast<size_t>(g.streams) * g.kv_heads * g.tiles * g.tile_bytes;
+}
+
+aqt_status aqt_cache_append(const float *qkv, int64_t T, int heads, const aqt_cache *cache, const int32_t *count, void *stream,
+                            int32_t *dev_status) {
+  AQT_TRY(cache_check(cache));
+  AQT_TRY(cache_call_check(cache, T, heads));
+  if (!qkv) return AQT_ERR_INVALID_ARG;
+  return launch_cache_append(qkv, T, heads, *cache, count, static_cast<hipStream_t>(stream), dev_status);
+}
+
+aqt_status aqt_cache_read(const aqt_cache *cache, int64_t pending, const int32_t *count, const int64_t *first, int64_t n, float *keys,
+                          float *values, void *stream) {
+  AQT_TRY(cache_check(cache));
+  if (!cache_buffers_ok(*cache) || pending < 0 || n < 1 || (!keys && !values)) return AQT_ERR_INVALID_ARG;
+  if (n > (int64_t(1) << 40) || pending > (int64_t(1) << 40)) return AQT_ERR_UNSUPPORTED;
+  return launch_cache_read(*cache, pending, count, first, n, keys, values, static_cast<hipStream_t>(stream));
+}
+
+aqt_status aqt_cache_advance(int64_t *length, int64_t streams, int64_t T, const int32_t *count, void *stream) {
+  if (!length || streams < 1 || T < 1) return AQT_ERR_INVALID_ARG;
+  if (streams > (int64_t(1) << 24) || T > (int64_t(1) << 40)) return AQT_ERR_UNSUPPORTED;
+  return launch_cache_advance(length, streams, T, count, static_cast<hipStream_t>(stream));
+}
+
+size_t aqt_attention_cached_workspace_bytes(const aqt_cache *cache, int64_t T, int heads) {
+  if (cache_check(cache) != AQT_OK || T < 1 || heads < 1 || heads % cache->kv_heads || !cached_attention_ok(*cache, T, heads)) return 0;
+  return cached_attention_ws_bytes(*cache, T, heads);
+}
+
+aqt_status aqt_attention_cached_fwd(const float *qkv, int64_t T, int heads, const aqt_cache *cache, const int32_t *count,
+                                    int left_context, int right_context, float *ctx, float *ctx_absmax, void *ws, size_t ws_bytes,
+                                    void *stream) {
+  AQT_TRY(cache_check(cache));
+  AQT_TRY(cache_call_check(cache, T, heads));
+  if (!qkv || !ctx) return AQT_ERR_INVALID_ARG;
+  if (!cached_attention_ok(*cache, T, heads)) return AQT_ERR_UNSUPPORTED;
+  const size_t rows = static_cast<size_t>(cache->streams) * T * cache->dh * sizeof(float);
+  if (overlap(qkv, rows * (heads + 2 * static_cast<size_t>(cache->kv_heads)), ctx, rows * heads)) return AQT_ERR_INVALID_ARG;
+  if (!ws || ws_bytes < cached_attention_ws_bytes(*cache, T, heads)) return AQT_ERR_WORKSPACE;
+  return launch_attention_cached(qkv, T, heads, *cache, count, left_context, right_context, ctx,
+                                 reinterpret_cast<uint32_t *>(ctx_absmax), ws, static_cast<hipStream_t>(stream));
 }
 
 }  // extern "C"

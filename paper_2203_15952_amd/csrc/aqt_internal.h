@@ -279,4 +279,12 @@ aqt_status launch_attention_bwd(const float *qkv, const float *ctx, const float 
                                 int64_t T, int64_t D, int heads, int left, int right, float *dqkv, void *ws,
                                 hipStream_t st);
 
+// ---- queries and keys normalised per head and rotated (rotate.hip) -----------------------------
+size_t rotate_bwd_ws_bytes(int dh);
+aqt_status launch_rotation_turns(int rot, double base, double *turns, hipStream_t st);
+aqt_status launch_rotate_fwd(const float *qkv, int64_t B, int64_t T, const aqt_qk_norm_rotate &s, const int64_t *first, float *out,
+                             hipStream_t st);
+aqt_status launch_rotate_bwd(const float *qkv, const float *dout, int64_t B, int64_t T, const aqt_qk_norm_rotate &s,
+                             const int64_t *first, float *dqkv, float *dgamma_q, float *dgamma_k, void *ws, hipStream_t st);
+
 }  // namespace aqt

@@ -1,0 +1,324 @@
+// Keys and values of a stream's new frames into its quantized cache, and back out of it (the layout is cache.h's).
+//
+// Writing, per frame and key / value head, separately for keys and values (Fig. 2 of arxiv 2203.15952, reduced over the head):
+//   scale = max|x| / qmax,   code = floor(x / scale + 0.5)   (0 where the scale is 0),   every operation one float32 rounding.
+// Reading: code * scale.  Memory bounds both: a frame's float32 row in one and its codes in the other direction.
+//
+// A group of L lanes takes four consecutive frames (aligned, so that they share a tile) of one head, a lane the same eight
+// columns of the four: a frame's maximum is L lanes' shuffles, a key row leaves (and comes) as dwords of four columns, and a
+// value row, whose four frames are neighbours, as dwords of four frames after a 4 x 4 transposition of bytes in registers.  Where a
+// call brings only some of the four frames the others' bytes are not touched.
+#include "cache.h"
+#include "quant_code.h"
+
+namespace aqt {
+namespace {
+
+constexpr int kThreads = 256;
+typedef float v4f __attribute__((ext_vector_type(4)));
+
+// Four dwords of four bytes each, transposed: out[i] byte f = in[f] byte i.
+__device__ __forceinline__ void transpose_bytes(uint32_t (&w)[4]) {
+  const uint32_t ab0 = __builtin_amdgcn_perm(w[1], w[0], 0x05010400u), ab1 = __builtin_amdgcn_perm(w[1], w[0], 0x07030602u);
+  const uint32_t cd0 = __builtin_amdgcn_perm(w[3], w[2], 0x05010400u), cd1 = __builtin_amdgcn_perm(w[3], w[2], 0x07030602u);
+  w[0] = __builtin_amdgcn_perm(cd0, ab0, 0x05040100u);
+  w[1] = __builtin_amdgcn_perm(cd0, ab0, 0x07060302u);
+  w[2] = __builtin_amdgcn_perm(cd1, ab1, 0x05040100u);
+  w[3] = __builtin_amdgcn_perm(cd1, ab1, 0x07060302u);
+}
+
+// What a group of lanes works on: four frames from `frame` (a multiple of four, possibly negative) of head h of stream b.
+struct Quad {
+  int64_t b, frame;
+  int h;
+  bool values, on;
+};
+// The quads of the frames from `from` on; items count (quad, keys or values, head), the last the fastest.
+__device__ __forceinline__ Quad quad_of(const CacheGeom &g, int64_t b, int item, int quads, int64_t from) {
+  const int per = 2 * g.kv_heads, q = item / per, w = item - q * per;
+  const bool values = w >= g.kv_heads;
+  return Quad{b, ((from >> 2) + q) * 4, values ? w - g.kv_heads : w, values, q < quads};
+}
+
+// A lane's eight columns: two times four.  Of a value row packed two to a byte they are 16 apart, otherwise 8, so that either
+// half of a byte is this lane's.
+struct Columns {
+  int lo, hi;
+  __device__ __forceinline__ Columns(int j, bool values)
+      : lo(values ? 32 * (j >> 2) + 4 * (j & 3) : 16 * (j >> 1) + 4 * (j & 1)), hi(lo + (values ? 16 : 8)) {}
+};
+
+__device__ __forceinline__ uint8_t *tile_of(const CacheGeom &g, const Quad &q) {
+  const int64_t at = (q.b * g.kv_heads + q.h) * g.tiles + tile_slot(q.frame >> 6, g.tiles);
+  return g.data + at * g.tile_bytes;
+}
+
+template <bool VEC>
+__device__ __forceinline__ void load4(float (&x)[4], const float *row, int col, int dh) {
+  if (VEC) {
+    if (col < dh) {
+      const v4f v = *reinterpret_cast<const v4f *>(row + col);
+      x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+    } else {
+      x[0] = x[1] = x[2] = x[3] = 0.0f;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = col + i < dh ? row[col + i] : 0.0f;
+  }
+}
+template <bool VEC>
+__device__ __forceinline__ void store4(const float (&x)[4], float *row, int col, int dh) {
+  if (VEC) {
+    if (col < dh) *reinterpret_cast<v4f *>(row + col) = v4f{x[0], x[1], x[2], x[3]};
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (col + i < dh) row[col + i] = x[i];
+  }
+}
+
+template <int L, bool VEC>
+__global__ __launch_bounds__(kThreads) void cache_append_kernel(const float *__restrict__ qkv, CacheGeom g, int64_t T, int heads,
+                                                                const int32_t *__restrict__ count, int quads, int blocks_per_stream,
+                                                                int32_t *__restrict__ dev_status) {
+  const int tid = static_cast<int>(threadIdx.x), j = tid % L;
+  const int64_t b = static_cast<int64_t>(blockIdx.x) / blocks_per_stream;
+  const int block = static_cast<int>(blockIdx.x) - static_cast<int>(b) * blocks_per_stream;
+  const StreamFrames f = stream_frames(g, count, T, b);
+  const int64_t from = f.length > f.oldest ? f.length : f.oldest;   // later frames of this call take the place of those before
+  const Quad q = quad_of(g, b, block * (kThreads / L) + tid / L, quads, from);
+  const bool live = q.on && from < f.end;
+  const int64_t ld = (static_cast<int64_t>(heads) + 2 * static_cast<int64_t>(g.kv_heads)) * g.dh;
+  const int64_t at = (heads + (q.values ? g.kv_heads : 0) + static_cast<int64_t>(q.h)) * g.dh;
+  const Columns c(j, q.values);
+  float x[4][2][4];
+  bool mine[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int64_t p = q.frame + i;
+    mine[i] = live && p >= from && p < f.end;
+    const int64_t t = mine[i] ? p - f.length : 0;   // always a row of the call
+    const float *const row = qkv + (b * T + t) * ld + at;
+    load4<VEC>(x[i][0], row, c.lo, g.dh);
+    load4<VEC>(x[i][1], row, c.hi, g.dh);
+  }
+  uint8_t *const tile = tile_of(g, q);
+  const int key = static_cast<int>(q.frame & 63);
+  uint32_t code[2][4];   // [half][frame]
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint32_t m = 0u;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) m = max(m, __float_as_uint(x[i][h][e]) & 0x7FFFFFFFu);
+#pragma unroll
+    for (int off = 1; off < L; off <<= 1) m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), off, 64)));
+    const float fq = static_cast<float>(g.qmax), s = __uint_as_float(m) / fq;
+    const Quantizer k = quantizer(s, fq);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) code[h][i] = quant4(x[i][h][0], x[i][h][1], x[i][h][2], x[i][h][3], k);
+    if (j == 0 && mine[i]) {
+      reinterpret_cast<float *>(tile + cache_scales(g))[(q.values ? 64 : 0) + key + i] = s;
+      if (dev_status && m >= 0x7F800000u) *dev_status = AQT_ERR_NONFINITE;
+    }
+  }
+  if (!q.values) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (!mine[i]) continue;
+      uint8_t *const row = tile + (key + i) * g.key_row;
+      if (g.packed) {
+        if (c.lo < 2 * g.key_row)
+          *reinterpret_cast<uint32_t *>(row + 8 * (j >> 1) + 4 * (j & 1)) = (code[0][i] & 0x0F0F0F0Fu) | (code[1][i] & 0x0F0F0F0Fu) << 4;
+      } else {
+        if (c.lo < g.key_row) *reinterpret_cast<uint32_t *>(row + c.lo) = code[0][i];
+        if (c.hi < g.key_row) *reinterpret_cast<uint32_t *>(row + c.hi) = code[1][i];
+      }
+    }
+    return;
+  }
+  transpose_bytes(code[0]);
+  transpose_bytes(code[1]);
+  uint8_t *const values = tile + cache_values(g) + frame_slot(key);
+  const bool whole = mine[0] && mine[1] && mine[2] && mine[3];
+  auto put = [&](int row, uint32_t w) {
+    if (row >= g.value_rows) return;
+    uint8_t *const at4 = values + row * 64;
+    if (whole) {
+      *reinterpret_cast<uint32_t *>(at4) = w;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (mine[i]) at4[i] = static_cast<uint8_t>(w >> (8 * i));
+    }
+  };
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    if (g.packed) {
+      put(16 * (j >> 2) + 4 * (j & 3) + e, (code[0][e] & 0x0F0F0F0Fu) | (code[1][e] & 0x0F0F0F0Fu) << 4);
+    } else {
+      put(c.lo + e, code[0][e]);
+      put(c.hi + e, code[1][e]);
+    }
+  }
+}
+
+// Four signed codes from a dword: bytes, or the low or high nibbles of bytes.
+__device__ __forceinline__ void codes_of(float (&x)[4], uint32_t w, bool packed, bool high) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const uint32_t byte = w >> (8 * e) & 0xFFu;
+    const int v = packed ? static_cast<int>((high ? byte >> 4 : byte) << 28) >> 28 : static_cast<int>(byte << 24) >> 24;
+    x[e] = static_cast<float>(v);
+  }
+}
+
+template <int L, bool VEC>
+__global__ __launch_bounds__(kThreads) void cache_read_kernel(CacheGeom g, int64_t pending, const int32_t *__restrict__ count,
+                                                              const int64_t *__restrict__ first, int64_t n, int quads,
+                                                              int blocks_per_stream, float *__restrict__ keys, float *__restrict__ values) {
+  const int tid = static_cast<int>(threadIdx.x), j = tid % L;
+  const int64_t b = static_cast<int64_t>(blockIdx.x) / blocks_per_stream;
+  const int block = static_cast<int>(blockIdx.x) - static_cast<int>(b) * blocks_per_stream;
+  const StreamFrames f = stream_frames(g, count, pending, b);
+  const int64_t far = int64_t(1) << 61;
+  int64_t from = first ? first[b] : f.end - n;
+  from = from < -far ? -far : from > far ? far : from;
+  const Quad q = quad_of(g, b, block * (kThreads / L) + tid / L, quads, from);
+  if (!q.on || q.frame >= from + n) return;
+  float *const to = q.values ? values : keys;
+  if (!to) return;
+  const Columns c(j, q.values);
+  bool held[4];
+  bool any = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    held[i] = q.frame + i >= f.oldest && q.frame + i < f.end;   // oldest is not negative
+    any = any || held[i];
+  }
+  uint32_t code[2][4] = {};   // [half][frame], packed: both halves in code[0]
+  float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+  if (any) {   // the tile is the cache's own whichever of its frames are held
+    const uint8_t *const tile = tile_of(g, q);
+    const int key = static_cast<int>(q.frame & 63);
+    const v4f scales = *reinterpret_cast<const v4f *>(tile + cache_scales(g) + 4 * ((q.values ? 64 : 0) + key));
+    s[0] = scales.x; s[1] = scales.y; s[2] = scales.z; s[3] = scales.w;
+    if (!q.values) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint8_t *const row = tile + (key + i) * g.key_row;
+        if (g.packed) {
+          if (c.lo < 2 * g.key_row) code[0][i] = *reinterpret_cast<const uint32_t *>(row + 8 * (j >> 1) + 4 * (j & 1));
+        } else {
+          if (c.lo < g.key_row) code[0][i] = *reinterpret_cast<const uint32_t *>(row + c.lo);
+          if (c.hi < g.key_row) code[1][i] = *reinterpret_cast<const uint32_t *>(row + c.hi);
+        }
+      }
+    } else {
+      const uint8_t *const at = tile + cache_values(g) + frame_slot(key);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int lo = g.packed ? 16 * (j >> 2) + 4 * (j & 3) + e : c.lo + e;
+        if (lo < g.value_rows) code[0][e] = *reinterpret_cast<const uint32_t *>(at + lo * 64);
+        if (!g.packed && c.hi + e < g.value_rows) code[1][e] = *reinterpret_cast<const uint32_t *>(at + (c.hi + e) * 64);
+      }
+      transpose_bytes(code[0]);
+      transpose_bytes(code[1]);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int64_t r = q.frame + i - from;
+    if (r < 0 || r >= n) continue;
+    float *const row = to + ((b * n + r) * g.kv_heads + q.h) * g.dh;
+    float x[2][4];
+    codes_of(x[0], code[0][i], g.packed, false);
+    codes_of(x[1], g.packed ? code[0][i] : code[1][i], g.packed, true);
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[h][e] = held[i] ? x[h][e] * s[i] : 0.0f;
+    store4<VEC>(x[0], row, c.lo, g.dh);
+    store4<VEC>(x[1], row, c.hi, g.dh);
+  }
+}
+
+__global__ void cache_advance_kernel(int64_t *__restrict__ length, int64_t streams, int64_t T, const int32_t *__restrict__ count) {
+  const int64_t b = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
+  if (b >= streams) return;
+  const int64_t n = count ? count[b] : T, L = length[b];
+  length[b] = (L < 0 ? 0 : L) + (n < 0 ? 0 : n > T ? T : n);
+}
+
+// Quads that `n` consecutive frames can touch, and the workgroups they make.
+int64_t quads_of(int64_t n) { return (n + 2) / 4 + 1; }
+int lanes_of(int dh) { return dh <= 32 ? 4 : dh <= 64 ? 8 : 16; }
+int64_t blocks_of(const CacheGeom &g, int64_t n) { return cdiv(quads_of(n) * 2 * g.kv_heads, kThreads / lanes_of(g.dh)); }
+// Items of a stream and workgroups of the launch count in 32 bits.
+bool grid_ok(const CacheGeom &g, int64_t n) {
+  return n <= (int64_t(1) << 40) && quads_of(n) * 2 * g.kv_heads <= INT32_MAX - kThreads && blocks_of(g, n) <= INT32_MAX / g.streams;
+}
+
+}  // namespace
+
+bool cache_shape_ok(const aqt_cache &c) {
+  return c.streams >= 1 && c.capacity >= 64 && c.capacity % 64 == 0 && c.capacity / 64 <= (1 << 24) && c.kv_heads >= 1 &&
+         c.kv_heads <= 4096 && c.dh >= 1 && c.dh <= 128 && bits_ok(c.bits) && c.streams <= (int64_t(1) << 24);
+}
+
+CacheGeom cache_geom(const aqt_cache &c) {
+  CacheGeom g;
+  const int d16 = static_cast<int>(align_up(c.dh, 16));
+  g.streams = c.streams;
+  g.tiles = static_cast<int>(c.capacity / 64);
+  g.kv_heads = c.kv_heads;
+  g.dh = c.dh;
+  g.qmax = qmax_of(c.bits);
+  g.packed = packed4(c.bits);
+  g.key_row = g.packed ? d16 / 2 : d16;
+  g.value_rows = g.packed ? 16 * static_cast<int>(cdiv(c.dh, 32)) : d16;
+  g.tile_bytes = 64 * (g.key_row + g.value_rows + 8);
+  g.data = static_cast<uint8_t *>(c.data);
+  g.length = c.length;
+  return g;
+}
+
+aqt_status launch_cache_append(const float *qkv, int64_t T, int heads, const aqt_cache &c, const int32_t *count, hipStream_t st,
+                               int32_t *dev_status) {
+  const CacheGeom g = cache_geom(c);
+  const int64_t most = T < c.capacity ? T : c.capacity, per = blocks_of(g, most);
+  if (!grid_ok(g, most)) return AQT_ERR_UNSUPPORTED;
+  const bool vec = reinterpret_cast<uintptr_t>(qkv) % 16 == 0 && c.dh % 4 == 0;
+  auto kern = c.dh <= 32   ? (vec ? cache_append_kernel<4, true> : cache_append_kernel<4, false>)
+              : c.dh <= 64 ? (vec ? cache_append_kernel<8, true> : cache_append_kernel<8, false>)
+                           : (vec ? cache_append_kernel<16, true> : cache_append_kernel<16, false>);
+  kern<<<static_cast<unsigned>(per * c.streams), kThreads, 0, st>>>(qkv, g, T, heads, count, static_cast<int>(quads_of(most)),
+                                                                   static_cast<int>(per), dev_status);
+  AQT_HIP(hipGetLastError());
+  return AQT_OK;
+}
+
+aqt_status launch_cache_read(const aqt_cache &c, int64_t pending, const int32_t *count, const int64_t *first, int64_t n, float *keys,
+                             float *values, hipStream_t st) {
+  const CacheGeom g = cache_geom(c);
+  const int64_t per = blocks_of(g, n);
+  if (!grid_ok(g, n)) return AQT_ERR_UNSUPPORTED;
+  const bool vec = reinterpret_cast<uintptr_t>(keys) % 16 == 0 && reinterpret_cast<uintptr_t>(values) % 16 == 0 && c.dh % 4 == 0;
+  auto kern = c.dh <= 32   ? (vec ? cache_read_kernel<4, true> : cache_read_kernel<4, false>)
+              : c.dh <= 64 ? (vec ? cache_read_kernel<8, true> : cache_read_kernel<8, false>)
+                           : (vec ? cache_read_kernel<16, true> : cache_read_kernel<16, false>);
+  kern<<<static_cast<unsigned>(per * c.streams), kThreads, 0, st>>>(g, pending, count, first, n, static_cast<int>(quads_of(n)),
+                                                                   static_cast<int>(per), keys, values);
+  AQT_HIP(hipGetLastError());
+  return AQT_OK;
+}
+
+aqt_status launch_cache_advance(int64_t *length, int64_t streams, int64_t T, const int32_t *count, hipStream_t st) {
+  cache_advance_kernel<<<static_cast<unsigned>(cdiv(streams, kThreads)), kThreads, 0, st>>>(length, streams, T, count);
+  AQT_HIP(hipGetLastError());
+  return AQT_OK;
+}
+
+}  // namespace aqt

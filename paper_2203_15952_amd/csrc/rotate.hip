@@ -1,0 +1,377 @@
+// Queries and keys of projected rows normalised per head and rotated by their frame's position, in one pass, and its gradient.
+// A row holds `heads` queries, `kv_heads` keys and `kv_heads` values of dh columns.  For every query and key head x:
+//   n = x / sqrt(mean(x^2) + eps) * gamma          (norm; gamma shared by the heads, one for queries, one for keys)
+//   (a, b) -> (a cos - b sin, a sin + b cos)       for the pairs (a, b) of the first `rot` columns, angle = 2 pi frame turns[i]
+// and backward, with u the upstream gradient rotated back by the same angles and x^ = x / sqrt(mean(x^2) + eps):
+//   dgamma = sum over rows and heads of u x^;   g = u gamma;   dx = (g - x^ mean(g x^)) / sqrt(mean(x^2) + eps).
+// The normaliser is formed again from x (it is in registers), so the forward keeps nothing.
+//
+// Memory bounds both directions: a row is read once and written once.  A group of LANES lanes owns one head at a time and a
+// lane the same columns of every head, so gamma, its gradient and the cosines stay in registers while the group walks the
+// heads of its row; a wavefront walks a run of rows.  A lane's columns are whole pairs, so rotating takes no exchange: for
+// halves (i, i + rot / 2) the 16-byte pieces at j and rot / 8 + j, for neighbours (2 i, 2 i + 1) two adjacent pieces.  Heads
+// that are not whole pieces, or not aligned, take single columns and shuffles for the partner (`Single`).
+//
+// The angle is exact where it matters: frame * turns in float64, reduced there to an eighth of a turn around the nearest
+// quarter, and only that remainder goes on in float32 (a position of a million frames costs no accuracy; in float32 its
+// angle would be off by 0.06).
+#include "aqt_internal.h"
+
+namespace aqt {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kBlocks = 2048;       // eight workgroups to a CU: 32 wavefronts
+constexpr int kFoldBlocks = 1024;   // ... where every workgroup leaves column sums behind
+typedef float v4f __attribute__((ext_vector_type(4)));
+
+struct RotateGeom {
+  int64_t T, M, ld;         // frames per utterance, rows, columns of a row
+  int heads, kv_heads, dh;
+  int rot;                  // columns that are rotated
+  int norm, in_place;       // in place: values are where they belong already
+  int per_row;              // groups of lanes that share a row: a power of two
+  float eps;
+  const double *turns;
+  const int64_t *first;     // nullable: frame number of every utterance's first row
+  const float *gamma[2];    // queries, keys; nullable
+};
+
+struct Angle {
+  float c, s;
+};
+
+// cos and sin of 2 pi x.  x = (quarter + r) / 4 with |r| <= 1/2; the Taylor polynomials' remainders at pi / 4 are 2e-9 (sine,
+// behind x^9) and 5e-11 (cosine, behind x^10).
+__device__ __forceinline__ Angle angle_of(double turn) {
+  const double q = rint(4.0 * turn);
+  const float r = static_cast<float>(4.0 * turn - q) * 1.57079632679489662f;
+  const int quarter = static_cast<int>(static_cast<int64_t>(q) & 3);
+  const float z = r * r;
+  float s = fmaf(z, 2.7557319224e-6f, -1.9841269841e-4f);
+  s = fmaf(z, s, 8.3333333333e-3f);
+  s = fmaf(z, s, -1.6666666667e-1f);
+  s = fmaf(r * z, s, r);
+  float c = fmaf(z, -2.7557319224e-7f, 2.4801587302e-5f);
+  c = fmaf(z, c, -1.3888888889e-3f);
+  c = fmaf(z, c, 4.1666666667e-2f);
+  c = fmaf(z, c, -0.5f);
+  c = fmaf(z, c, 1.0f);
+  const float cc = quarter & 1 ? s : c, ss = quarter & 1 ? c : s;
+  return Angle{quarter == 1 || quarter == 2 ? -cc : cc, quarter >= 2 ? -ss : ss};
+}
+
+// Eight columns of a head in two 16-byte pieces: lane j of the group.
+template <int L, bool HALVES>
+struct Pieces {
+  static constexpr int LANES = L, N = 8, ANGLES = 4;
+  int at[2];       // the pieces' first columns
+  bool has[2];
+  int pair;        // the first of this lane's four pairs
+  int pairs;       // ... and how many of them are rotated
+  __device__ __forceinline__ Pieces(int j, int dh, int rot) {
+    const int half = rot >> 3;   // pieces in half of the rotated columns
+    pair = 4 * j;
+    pairs = (rot >> 1) - pair;
+    if (HALVES) {
+      at[0] = j < half ? 4 * j : 8 * j;            // behind the rotated ones: pieces 2 half + 2 (j - half)
+      at[1] = j < half ? 4 * (j + half) : at[0] + 4;
+    } else {
+      at[0] = 8 * j;
+      at[1] = 8 * j + 4;
+    }
+    has[0] = at[0] < dh;
+    has[1] = at[1] < dh;
+  }
+  __device__ __forceinline__ int column(int i) const { return at[i >> 2] + (i & 3); }
+  __device__ __forceinline__ bool own(int i) const { return has[i >> 2]; }
+  __device__ __forceinline__ bool rotated(int i) const { return i < pairs; }
+  __device__ __forceinline__ int pair_of(int i) const { return pair + i; }
+  __device__ __forceinline__ void load(float (&x)[N], const float *p, bool on) const {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      v4f v = {0.0f, 0.0f, 0.0f, 0.0f};
+      if (on && has[h]) v = *reinterpret_cast<const v4f *>(p + at[h]);
+      x[4 * h] = v.x; x[4 * h + 1] = v.y; x[4 * h + 2] = v.z; x[4 * h + 3] = v.w;
+    }
+  }
+  __device__ __forceinline__ void store(const float (&x)[N], float *p) const {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      if (has[h]) *reinterpret_cast<v4f *>(p + at[h]) = v4f{x[4 * h], x[4 * h + 1], x[4 * h + 2], x[4 * h + 3]};
+  }
+  __device__ __forceinline__ void turn(float (&x)[N], const Angle (&t)[ANGLES], bool back) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int ia = HALVES ? i : 2 * i, ib = HALVES ? i + 4 : 2 * i + 1;
+      const float a = x[ia], b = x[ib], s = back ? -t[i].s : t[i].s;
+      x[ia] = i < pairs ? a * t[i].c - b * s : a;
+      x[ib] = i < pairs ? a * s + b * t[i].c : b;
+    }
+  }
+};
+
+// Two columns of a head, j and j + L: any head width and alignment.
+template <int L, bool HALVES>
+struct Single {
+  static constexpr int LANES = L, N = 2, ANGLES = 2;
+  int j, dh, rot;
+  __device__ __forceinline__ Single(int j_, int dh_, int rot_) : j(j_), dh(dh_), rot(rot_) {}
+  __device__ __forceinline__ int column(int i) const { return j + L * i; }
+  __device__ __forceinline__ bool own(int i) const { return column(i) < dh; }
+  __device__ __forceinline__ bool rotated(int i) const { return column(i) < rot; }
+  __device__ __forceinline__ int pair_of(int i) const {
+    const int c = column(i);
+    return HALVES ? (c < (rot >> 1) ? c : c - (rot >> 1)) : c >> 1;
+  }
+  __device__ __forceinline__ void load(float (&x)[N], const float *p, bool on) const {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) x[i] = on && own(i) ? p[column(i)] : 0.0f;
+  }
+  __device__ __forceinline__ void store(const float (&x)[N], float *p) const {
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      if (own(i)) p[column(i)] = x[i];
+  }
+  __device__ __forceinline__ void turn(float (&x)[N], const Angle (&t)[ANGLES], bool back) const {
+    const int base = static_cast<int>(threadIdx.x & 63u) - j, half = rot >> 1;
+    float y[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int c = column(i);
+      const bool second = HALVES ? c >= half : c & 1;
+      const int p = c >= rot ? c : HALVES ? (second ? c - half : c + half) : c ^ 1;   // the partner's column
+      const float lo = __shfl(x[0], base + (p & (L - 1))), hi = __shfl(x[1], base + (p & (L - 1)));
+      const float other = p < L ? lo : hi, s = back ? -t[i].s : t[i].s;
+      y[i] = c >= rot ? x[i] : second ? other * s + x[i] * t[i].c : x[i] * t[i].c - other * s;
+    }
+    x[0] = y[0];
+    x[1] = y[1];
+  }
+};
+
+template <int L>
+__device__ __forceinline__ float group_sum(float v) {
+#pragma unroll
+  for (int off = 1; off < L; off <<= 1) v += __shfl_xor(v, off, 64);
+  return v;
+}
+
+// BWD: y is the upstream gradient, out the gradient with respect to x, part (nullable) [workgroups][2][dh] column sums.
+template <class F, bool BWD>
+__global__ __launch_bounds__(kThreads) void rotate_kernel(const float *x, const float *y, RotateGeom g, float *out, float *part) {
+  constexpr int L = F::LANES, N = F::N, GROUPS = 64 / L;
+  const int tid = static_cast<int>(threadIdx.x), lane = tid & 63, group = lane / L, j = lane % L;
+  const F f(j, g.dh, g.rot);
+  const int sub = group % g.per_row, row_of = group / g.per_row, rows_at_once = GROUPS / g.per_row;
+  const int turned = g.heads + g.kv_heads, all = turned + (g.in_place ? 0 : g.kv_heads);
+
+  float gain[2][N], dgain[2][N];
+#pragma unroll
+  for (int w = 0; w < 2; ++w)
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      gain[w][i] = g.gamma[w] && f.own(i) ? g.gamma[w][f.column(i)] : 1.0f;
+      dgain[w][i] = 0.0f;
+    }
+  double rate[F::ANGLES];
+#pragma unroll
+  for (int i = 0; i < F::ANGLES; ++i) rate[i] = f.rotated(i) ? g.turns[f.pair_of(i)] : 0.0;
+
+  // this wavefront's run of rows
+  const int64_t wave = static_cast<int64_t>(blockIdx.x) * (kThreads / 64) + (tid >> 6), waves = static_cast<int64_t>(gridDim.x) * (kThreads / 64);
+  const int64_t runs = cdiv(g.M, rows_at_once), each = cdiv(runs, waves);
+  const int64_t begin = wave * each * rows_at_once, end = begin + each * rows_at_once < g.M ? begin + each * rows_at_once : g.M;
+  const float inv = 1.0f / static_cast<float>(g.dh);
+  int64_t b = 0, t = 0;
+  if (begin < end) {
+    b = (begin + row_of) / g.T;
+    t = (begin + row_of) - b * g.T;
+  }
+  for (int64_t m0 = begin; m0 < end; m0 += rows_at_once) {
+    const int64_t m = m0 + row_of;
+    const bool row_ok = m < end;
+    const double frame = row_ok ? static_cast<double>((g.first ? g.first[b] : 0) + t) : 0.0;
+    Angle a[F::ANGLES];
+#pragma unroll
+    for (int i = 0; i < F::ANGLES; ++i) a[i] = angle_of(frame * rate[i]);
+    const float *const xr = x + m * g.ld, *const yr = BWD ? y + m * g.ld : nullptr;
+    float *const outr = out + m * g.ld;
+    for (int h0 = 0; h0 < all; h0 += g.per_row) {   // the same number of steps for every lane of the wavefront
+      const int h = h0 + sub;
+      const bool on = row_ok && h < all, value = h >= turned;
+      const int64_t at = static_cast<int64_t>(h) * g.dh;
+      float v[N], u[N];
+      if (!BWD) {
+        f.load(v, xr + at, on);
+        if (g.norm) {
+          float ss = 0.0f;
+#pragma unroll
+          for (int i = 0; i < N; ++i) ss = fmaf(v[i], v[i], ss);
+          const float r = 1.0f / sqrtf(group_sum<L>(ss) * inv + g.eps);
+#pragma unroll
+          for (int i = 0; i < N; ++i) u[i] = v[i] * r * (h < g.heads ? gain[0][i] : gain[1][i]);
+        } else {
+#pragma unroll
+          for (int i = 0; i < N; ++i) u[i] = v[i];
+        }
+        f.turn(u, a, false);
+#pragma unroll
+        for (int i = 0; i < N; ++i) u[i] = value ? v[i] : u[i];
+      } else {
+        float w[N];
+        f.load(w, yr + at, on);
+#pragma unroll
+        for (int i = 0; i < N; ++i) u[i] = w[i];
+        f.turn(u, a, true);
+        if (g.norm) {
+          f.load(v, xr + at, on && !value);
+          float ss = 0.0f;
+#pragma unroll
+          for (int i = 0; i < N; ++i) ss = fmaf(v[i], v[i], ss);
+          const float r = 1.0f / sqrtf(group_sum<L>(ss) * inv + g.eps);
+          float dot = 0.0f;
+#pragma unroll
+          for (int i = 0; i < N; ++i) {
+            v[i] *= r;
+            const float mine = on && !value ? u[i] * v[i] : 0.0f;
+            dgain[0][i] += h < g.heads ? mine : 0.0f;
+            dgain[1][i] += h < g.heads ? 0.0f : mine;
+            u[i] *= h < g.heads ? gain[0][i] : gain[1][i];
+            dot = fmaf(u[i], v[i], dot);
+          }
+          dot = group_sum<L>(dot) * inv;
+#pragma unroll
+          for (int i = 0; i < N; ++i) u[i] = (u[i] - v[i] * dot) * r;
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) u[i] = value ? w[i] : u[i];
+      }
+      if (on) f.store(u, outr + at);
+    }
+    t += rows_at_once;
+    while (t >= g.T) {   // at most rows_at_once times
+      t -= g.T;
+      ++b;
+    }
+  }
+  if constexpr (BWD) {
+    if (!part) return;
+    // over the groups of the wavefront, then over the wavefronts
+    __shared__ float sums[kThreads / 64][2][128];
+#pragma unroll
+    for (int w = 0; w < 2; ++w)
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        float s = dgain[w][i];
+#pragma unroll
+        for (int off = L; off < 64; off <<= 1) s += __shfl_xor(s, off, 64);
+        if (group == 0 && f.own(i)) sums[tid >> 6][w][f.column(i)] = s;
+      }
+    __syncthreads();
+    if (tid < 2 * g.dh) {
+      const int w = tid >= g.dh, c = w ? tid - g.dh : tid;
+      float s = 0.0f;
+      for (int k = 0; k < kThreads / 64; ++k) s += sums[k][w][c];
+      part[static_cast<int64_t>(blockIdx.x) * 2 * g.dh + tid] = s;
+    }
+  }
+}
+
+// dgamma[c] = sum over workgroups, in a fixed order, in float64: sixteen columns to a workgroup, sixteen threads to a column
+__global__ __launch_bounds__(kThreads) void rotate_fold_kernel(const float *__restrict__ part, int parts, int dh, float *__restrict__ dgq,
+                                                               float *__restrict__ dgk) {
+  __shared__ double sums[16][16];
+  const int c = static_cast<int>(blockIdx.x) * 16 + static_cast<int>(threadIdx.x & 15u), slice = static_cast<int>(threadIdx.x >> 4);
+  double s = 0.0;
+  if (c < 2 * dh)
+    for (int p = slice; p < parts; p += 16) s += static_cast<double>(part[static_cast<int64_t>(p) * 2 * dh + c]);
+  sums[slice][threadIdx.x & 15u] = s;
+  __syncthreads();
+  if (slice == 0 && c < 2 * dh) {
+    for (int k = 1; k < 16; ++k) s += sums[k][threadIdx.x & 15u];
+    float *const to = c < dh ? dgq : dgk;
+    if (to) to[c < dh ? c : c - dh] = static_cast<float>(s);
+  }
+}
+
+__global__ void rotation_turns_kernel(int pairs, double log2_base, double *__restrict__ turns) {
+  const int i = static_cast<int>(threadIdx.x);
+  if (i < pairs) turns[i] = exp2(-log2_base * static_cast<double>(i) / static_cast<double>(pairs)) * 0.15915494309189533577;
+}
+
+unsigned rotate_blocks(int64_t M, int rows_at_once, int most) {
+  const int64_t want = cdiv(cdiv(M, rows_at_once), kThreads / 64);
+  return static_cast<unsigned>(want < most ? want : most);
+}
+
+template <class F, bool BWD>
+aqt_status launch_as(const float *x, const float *y, RotateGeom g, float *out, float *part, hipStream_t st, unsigned *blocks) {
+  g.per_row = 1;   // by all heads, in place too: the same lanes add up the same terms
+  while (g.per_row < 64 / F::LANES && g.per_row < g.heads + 2 * g.kv_heads) g.per_row *= 2;
+  *blocks = rotate_blocks(g.M, 64 / F::LANES / g.per_row, part ? kFoldBlocks : kBlocks);
+  rotate_kernel<F, BWD><<<*blocks, kThreads, 0, st>>>(x, y, g, out, part);
+  AQT_HIP(hipGetLastError());
+  return AQT_OK;
+}
+
+template <bool HALVES, bool BWD>
+aqt_status launch_paired(const float *x, const float *y, const RotateGeom &g, float *out, float *part, bool aligned, hipStream_t st,
+                         unsigned *blocks) {
+  // whole 16-byte pieces; in halves the rotated columns are whole pieces in either half too
+  if (aligned && g.dh % 4 == 0 && (!HALVES || g.rot % 8 == 0)) {
+    if (g.dh <= 32) return launch_as<Pieces<4, HALVES>, BWD>(x, y, g, out, part, st, blocks);
+    if (g.dh <= 64) return launch_as<Pieces<8, HALVES>, BWD>(x, y, g, out, part, st, blocks);
+    return launch_as<Pieces<16, HALVES>, BWD>(x, y, g, out, part, st, blocks);
+  }
+  if (g.dh <= 32) return launch_as<Single<16, HALVES>, BWD>(x, y, g, out, part, st, blocks);
+  return launch_as<Single<64, HALVES>, BWD>(x, y, g, out, part, st, blocks);
+}
+
+RotateGeom rotate_geom(int64_t B, int64_t T, const aqt_qk_norm_rotate &s, const int64_t *first, bool in_place) {
+  RotateGeom g;
+  g.T = T; g.M = B * T;
+  g.ld = (static_cast<int64_t>(s.heads) + 2 * static_cast<int64_t>(s.kv_heads)) * s.dh;
+  g.heads = s.heads; g.kv_heads = s.kv_heads; g.dh = s.dh; g.rot = s.rot;
+  g.norm = s.norm; g.in_place = in_place; g.per_row = 1;
+  g.eps = s.eps; g.turns = s.turns; g.first = first;
+  g.gamma[0] = s.gamma_q; g.gamma[1] = s.gamma_k;
+  return g;
+}
+
+bool aligned16(const void *p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+}  // namespace
+
+size_t rotate_bwd_ws_bytes(int dh) { return align_up(static_cast<size_t>(kFoldBlocks) * 2 * dh * sizeof(float), 256); }
+
+aqt_status launch_rotation_turns(int rot, double base, double *turns, hipStream_t st) {
+  rotation_turns_kernel<<<1, 64, 0, st>>>(rot / 2, log2(base), turns);
+  AQT_HIP(hipGetLastError());
+  return AQT_OK;
+}
+
+aqt_status launch_rotate_fwd(const float *qkv, int64_t B, int64_t T, const aqt_qk_norm_rotate &s, const int64_t *first, float *out,
+                             hipStream_t st) {
+  const RotateGeom g = rotate_geom(B, T, s, first, out == qkv);
+  const bool al = aligned16(qkv) && aligned16(out);
+  unsigned blocks;
+  return s.pairing == AQT_ROTATE_HALVES ? launch_paired<true, false>(qkv, nullptr, g, out, nullptr, al, st, &blocks)
+                                        : launch_paired<false, false>(qkv, nullptr, g, out, nullptr, al, st, &blocks);
+}
+
+aqt_status launch_rotate_bwd(const float *qkv, const float *dout, int64_t B, int64_t T, const aqt_qk_norm_rotate &s, const int64_t *first,
+                             float *dqkv, float *dgamma_q, float *dgamma_k, void *ws, hipStream_t st) {
+  const RotateGeom g = rotate_geom(B, T, s, first, dqkv == dout);
+  const bool al = aligned16(dout) && aligned16(dqkv) && aligned16(qkv);
+  float *const part = dgamma_q || dgamma_k ? static_cast<float *>(ws) : nullptr;
+  unsigned blocks;
+  AQT_TRY((s.pairing == AQT_ROTATE_HALVES ? launch_paired<true, true>(qkv, dout, g, dqkv, part, al, st, &blocks)
+                                          : launch_paired<false, true>(qkv, dout, g, dqkv, part, al, st, &blocks)));
+  if (!part) return AQT_OK;
+  rotate_fold_kernel<<<static_cast<unsigned>(cdiv(2 * s.dh, 16)), kThreads, 0, st>>>(part, static_cast<int>(blocks), s.dh, dgamma_q, dgamma_k);
+  AQT_HIP(hipGetLastError());
+  return AQT_OK;
+}
+
+}  // namespace aqt

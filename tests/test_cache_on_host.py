@@ -1,0 +1,43 @@
+"""The kernels of the quantized cache, of the attention over it and of the rotation of queries and keys run on the host, thread by
+thread, under the address and undefined-behaviour sanitizers, against float64 loops: every access of rings that wrap, ragged
+batches, odd heads and tiles with both ends inside is checked against buffers of exactly their size."""
+import os
+import subprocess
+
+import pytest
+
+from test_kernels_on_host import HERE, ROOT, read, rule
+
+
+def spliced():
+    def kernels(name, space, until):
+        src = read(name).replace("namespace aqt {\nnamespace {", "namespace aqt {\nnamespace %s {" % space, 1)
+        return src[:src.index(until)] + "}\n}\n"
+
+    layout = read("cache.h")
+    layout = layout[:layout.index("bool cache_shape_ok")] + rule("cache.hip", "CacheGeom cache_geom(") + "}\n"
+    helpers = "namespace aqt {\n" + "".join(rule_line + "\n" for rule_line in (
+        "inline int qmax_of(int bits) { return (1 << (bits - 1)) - 1; }", "inline bool packed4(int bits_w) { return bits_w <= 4; }")) + "}\n"
+    shim = ('#define AQT_ON_HOST 1\n#include "vectors_on_host.h"\n#include "aqt.h"\n'
+            "inline float __shfl(float v, int lane) { return lane_value(v, (unsigned)lane); }\n")
+    return (shim + helpers + layout + read("quant_code.h") + kernels("cache.hip", "cache_", "}  // namespace\n\nbool cache_shape_ok") +
+            kernels("attention_cached.hip", "attend", "// Workgroups that share the tiles of 16 rows.") +
+            kernels("rotate.hip", "turn", "__global__ void rotation_turns_kernel") +
+            open(os.path.join(HERE, "host_emulation", "cache_driver.cpp")).read())
+
+
+@pytest.fixture(scope="module")
+def exe(tmp_path_factory):
+    path = tmp_path_factory.mktemp("cache_on_host")
+    (path / "cache.cpp").write_text(spliced())
+    r = subprocess.run(["g++", "-O1", "-g", "-fsanitize=address,undefined", "-fno-sanitize-recover=all", "-static-libasan", "-static-libubsan",
+                        "-std=c++20", "-pthread", "-I", os.path.join(HERE, "host_emulation"), "-I", os.path.join(ROOT, "include"),
+                        str(path / "cache.cpp"), "-o", str(path / "cache")], capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr[-3000:]
+    return str(path / "cache")
+
+
+@pytest.mark.parametrize("what", [[], ["rotate"]], ids=["cache", "rotate"])
+def test_kernels_in_bounds_and_correct_on_host(exe, what):
+    r = subprocess.run([exe, *what], capture_output=True, text=True, env=dict(os.environ, ASAN_OPTIONS="detect_leaks=0"), timeout=900)
+    assert r.returncode == 0 and r.stdout.strip().endswith("ok"), (r.stdout[-3000:], r.stderr[-3000:])
