@@ -23,6 +23,8 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kBlocks = 2048;       // eight workgroups to a CU: 32 wavefronts
 constexpr int kFoldBlocks = 1024;   // ... where every workgroup leaves column sums behind
+constexpr int kFwdHeads = 2, kBwdHeads = 1;   // heads of a lane whose loads are in flight together
+constexpr int kMaxPairs = 64;                 // of the widest head
 typedef float v4f __attribute__((ext_vector_type(4)));
 
 struct RotateGeom {
@@ -31,13 +33,14 @@ struct RotateGeom {
   int rot;                  // columns that are rotated
   int norm, in_place;       // in place: values are where they belong already
   int per_row;              // groups of lanes that share a row: a power of two
+  int64_t each;             // rows of a wavefront's run
   float eps;
   const double *turns;
   const int64_t *first;     // nullable: frame number of every utterance's first row
   const float *gamma[2];    // queries, keys; nullable
 };
 
-struct Angle {
+struct __attribute__((aligned(8))) Angle {
   float c, s;
 };
 
@@ -46,7 +49,7 @@ struct Angle {
 __device__ __forceinline__ Angle angle_of(double turn) {
   const double q = rint(4.0 * turn);
   const float r = static_cast<float>(4.0 * turn - q) * 1.57079632679489662f;
-  const int quarter = static_cast<int>(static_cast<int64_t>(q) & 3);
+  const int quarter = static_cast<int>(q - 4.0 * rint(0.25 * q)) & 3;   // -2 .. 2, mod 4
   const float z = r * r;
   float s = fmaf(z, 2.7557319224e-6f, -1.9841269841e-4f);
   s = fmaf(z, s, 8.3333333333e-3f);
@@ -64,7 +67,7 @@ __device__ __forceinline__ Angle angle_of(double turn) {
 // Eight columns of a head in two 16-byte pieces: lane j of the group.
 template <int L, bool HALVES>
 struct Pieces {
-  static constexpr int LANES = L, N = 8, ANGLES = 4;
+  static constexpr int LANES = L, N = 8, ANGLES = 4, PAIRS = 4 * L;   // PAIRS: of a head, at most
   int at[2];       // the pieces' first columns
   bool has[2];
   int pair;        // the first of this lane's four pairs
@@ -85,13 +88,19 @@ struct Pieces {
   }
   __device__ __forceinline__ int column(int i) const { return at[i >> 2] + (i & 3); }
   __device__ __forceinline__ bool own(int i) const { return has[i >> 2]; }
-  __device__ __forceinline__ bool rotated(int i) const { return i < pairs; }
   __device__ __forceinline__ int pair_of(int i) const { return pair + i; }
   __device__ __forceinline__ void load(float (&x)[N], const float *p, bool on) const {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
       v4f v = {0.0f, 0.0f, 0.0f, 0.0f};
       if (on && has[h]) v = *reinterpret_cast<const v4f *>(p + at[h]);
+      x[4 * h] = v.x; x[4 * h + 1] = v.y; x[4 * h + 2] = v.z; x[4 * h + 3] = v.w;
+    }
+  }
+  __device__ __forceinline__ void load_gains(float (&x)[N], const float *p) const {   // 128 of them, whatever the head
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const v4f v = *reinterpret_cast<const v4f *>(p + (has[h] ? at[h] : 0));
       x[4 * h] = v.x; x[4 * h + 1] = v.y; x[4 * h + 2] = v.z; x[4 * h + 3] = v.w;
     }
   }
@@ -114,19 +123,22 @@ struct Pieces {
 // Two columns of a head, j and j + L: any head width and alignment.
 template <int L, bool HALVES>
 struct Single {
-  static constexpr int LANES = L, N = 2, ANGLES = 2;
+  static constexpr int LANES = L, N = 2, ANGLES = 2, PAIRS = L;
   int j, dh, rot;
   __device__ __forceinline__ Single(int j_, int dh_, int rot_) : j(j_), dh(dh_), rot(rot_) {}
   __device__ __forceinline__ int column(int i) const { return j + L * i; }
   __device__ __forceinline__ bool own(int i) const { return column(i) < dh; }
-  __device__ __forceinline__ bool rotated(int i) const { return column(i) < rot; }
   __device__ __forceinline__ int pair_of(int i) const {
     const int c = column(i);
-    return HALVES ? (c < (rot >> 1) ? c : c - (rot >> 1)) : c >> 1;
+    return c >= rot ? 0 : HALVES ? (c < (rot >> 1) ? c : c - (rot >> 1)) : c >> 1;
   }
   __device__ __forceinline__ void load(float (&x)[N], const float *p, bool on) const {
 #pragma unroll
     for (int i = 0; i < 2; ++i) x[i] = on && own(i) ? p[column(i)] : 0.0f;
+  }
+  __device__ __forceinline__ void load_gains(float (&x)[N], const float *p) const {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) x[i] = p[own(i) ? column(i) : 0];
   }
   __device__ __forceinline__ void store(const float (&x)[N], float *p) const {
 #pragma unroll
@@ -160,94 +172,125 @@ __device__ __forceinline__ float group_sum(float v) {
 // BWD: y is the upstream gradient, out the gradient with respect to x, part (nullable) [workgroups][2][dh] column sums.
 template <class F, bool BWD>
 __global__ __launch_bounds__(kThreads) void rotate_kernel(const float *x, const float *y, RotateGeom g, float *out, float *part) {
-  constexpr int L = F::LANES, N = F::N, GROUPS = 64 / L;
+  constexpr int L = F::LANES, N = F::N, GROUPS = 64 / L, U = BWD ? kBwdHeads : kFwdHeads, PAIRS = F::PAIRS;
   const int tid = static_cast<int>(threadIdx.x), lane = tid & 63, group = lane / L, j = lane % L;
   const F f(j, g.dh, g.rot);
   const int sub = group % g.per_row, row_of = group / g.per_row, rows_at_once = GROUPS / g.per_row;
   const int turned = g.heads + g.kv_heads, all = turned + (g.in_place ? 0 : g.kv_heads);
 
-  float gain[2][N], dgain[2][N];
+  // In LDS: gains and turns (in registers they cost the kernel half of its wavefronts), and the angles of a row, which the lanes
+  // that share it form once between them.
+  __shared__ __attribute__((aligned(16))) float gains[2][128];
+  __shared__ double turns[kMaxPairs];
+  __shared__ Angle angles[kThreads / 64][64 * 4];
+  if (tid < 2 * 128) {
+    const int w = tid >> 7, c = tid & 127;
+    gains[w][c] = g.gamma[w] && c < g.dh ? g.gamma[w][c] : 1.0f;
+  }
+  if (tid < kMaxPairs) turns[tid] = tid < g.rot / 2 ? g.turns[tid] : 0.0;
+  const int row_lanes = L * g.per_row, place = sub * L + j;
+  Angle *const row_angles = angles[tid >> 6] + row_of * PAIRS;
+  float dgain[2][N];   // only where it is asked for (BWD)
 #pragma unroll
   for (int w = 0; w < 2; ++w)
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-      gain[w][i] = g.gamma[w] && f.own(i) ? g.gamma[w][f.column(i)] : 1.0f;
-      dgain[w][i] = 0.0f;
-    }
-  double rate[F::ANGLES];
-#pragma unroll
-  for (int i = 0; i < F::ANGLES; ++i) rate[i] = f.rotated(i) ? g.turns[f.pair_of(i)] : 0.0;
+    for (int i = 0; i < N; ++i) dgain[w][i] = 0.0f;
+  __syncthreads();
 
   // this wavefront's run of rows
-  const int64_t wave = static_cast<int64_t>(blockIdx.x) * (kThreads / 64) + (tid >> 6), waves = static_cast<int64_t>(gridDim.x) * (kThreads / 64);
-  const int64_t runs = cdiv(g.M, rows_at_once), each = cdiv(runs, waves);
-  const int64_t begin = wave * each * rows_at_once, end = begin + each * rows_at_once < g.M ? begin + each * rows_at_once : g.M;
+  const int64_t wave = static_cast<int64_t>(blockIdx.x) * (kThreads / 64) + (tid >> 6);
+  const int64_t begin = wave * g.each, end = begin + g.each < g.M ? begin + g.each : g.M;
   const float inv = 1.0f / static_cast<float>(g.dh);
-  int64_t b = 0, t = 0;
-  if (begin < end) {
-    b = (begin + row_of) / g.T;
-    t = (begin + row_of) - b * g.T;
+  const int64_t own = begin + row_of;
+  int64_t b, t;
+  if (g.M >> 31 == 0) {   // (a divide of 64 bits takes longer than the rest of a short call)
+    const uint32_t q = static_cast<uint32_t>(own) / static_cast<uint32_t>(g.T);
+    b = q;
+    t = static_cast<uint32_t>(own) - q * static_cast<uint32_t>(g.T);
+  } else {
+    b = own / g.T;
+    t = own - b * g.T;
   }
   for (int64_t m0 = begin; m0 < end; m0 += rows_at_once) {
     const int64_t m = m0 + row_of;
     const bool row_ok = m < end;
     const double frame = row_ok ? static_cast<double>((g.first ? g.first[b] : 0) + t) : 0.0;
-    Angle a[F::ANGLES];
-#pragma unroll
-    for (int i = 0; i < F::ANGLES; ++i) a[i] = angle_of(frame * rate[i]);
     const float *const xr = x + m * g.ld, *const yr = BWD ? y + m * g.ld : nullptr;
     float *const outr = out + m * g.ld;
-    for (int h0 = 0; h0 < all; h0 += g.per_row) {   // the same number of steps for every lane of the wavefront
-      const int h = h0 + sub;
-      const bool on = row_ok && h < all, value = h >= turned;
-      const int64_t at = static_cast<int64_t>(h) * g.dh;
-      float v[N], u[N];
-      if (!BWD) {
-        f.load(v, xr + at, on);
-        if (g.norm) {
-          float ss = 0.0f;
+    Angle a[F::ANGLES];
+    for (int h0 = 0; h0 < all; h0 += U * g.per_row) {   // the same number of steps for every lane of the wavefront
+      // U heads at a time, all of their loads in front of what is computed
+      float v[U][N], w[U][N];
 #pragma unroll
-          for (int i = 0; i < N; ++i) ss = fmaf(v[i], v[i], ss);
-          const float r = 1.0f / sqrtf(group_sum<L>(ss) * inv + g.eps);
+      for (int k = 0; k < U; ++k) {
+        const int h = h0 + k * g.per_row + sub;
+        const bool on = row_ok && h < all;
+        const int64_t at = static_cast<int64_t>(h) * g.dh;
+        if (BWD) f.load(w[k], yr + at, on);
+        if (!BWD || g.norm) f.load(v[k], xr + at, on && (!BWD || h < turned));
+      }
+      if (h0 == 0) {
+#pragma unroll 1
+        for (int at = place; at < PAIRS; at += row_lanes) row_angles[at] = angle_of(frame * turns[at]);
+        wave_lds_order();
 #pragma unroll
-          for (int i = 0; i < N; ++i) u[i] = v[i] * r * (h < g.heads ? gain[0][i] : gain[1][i]);
+        for (int i = 0; i < F::ANGLES; ++i) a[i] = row_angles[f.pair_of(i)];
+        wave_lds_order();   // read before the next row's are written
+      }
+#pragma unroll
+      for (int k = 0; k < U; ++k) {
+        if (h0 + k * g.per_row >= all) break;
+        const int h = h0 + k * g.per_row + sub;
+        const bool on = row_ok && h < all, value = h >= turned, query = h < g.heads;
+        float u[N];
+        if (h0 + k * g.per_row >= turned) {   // nothing but values
+#pragma unroll
+          for (int i = 0; i < N; ++i) u[i] = BWD ? w[k][i] : v[k][i];
+        } else if (!BWD) {
+          if (g.norm) {
+            float gain[N], ss = 0.0f;
+            f.load_gains(gain, gains[query ? 0 : 1]);
+#pragma unroll
+            for (int i = 0; i < N; ++i) ss = fmaf(v[k][i], v[k][i], ss);
+            const float r = __builtin_amdgcn_rsqf(group_sum<L>(ss) * inv + g.eps);
+#pragma unroll
+            for (int i = 0; i < N; ++i) u[i] = v[k][i] * r * gain[i];
+          } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i) u[i] = v[k][i];
+          }
+          f.turn(u, a, false);
+#pragma unroll
+          for (int i = 0; i < N; ++i) u[i] = value ? v[k][i] : u[i];
         } else {
 #pragma unroll
-          for (int i = 0; i < N; ++i) u[i] = v[i];
-        }
-        f.turn(u, a, false);
+          for (int i = 0; i < N; ++i) u[i] = w[k][i];
+          f.turn(u, a, true);
+          if (g.norm) {
+            float gain[N], ss = 0.0f;
+            f.load_gains(gain, gains[query ? 0 : 1]);
 #pragma unroll
-        for (int i = 0; i < N; ++i) u[i] = value ? v[i] : u[i];
-      } else {
-        float w[N];
-        f.load(w, yr + at, on);
+            for (int i = 0; i < N; ++i) ss = fmaf(v[k][i], v[k][i], ss);
+            const float r = __builtin_amdgcn_rsqf(group_sum<L>(ss) * inv + g.eps);
+            float dot = 0.0f;
 #pragma unroll
-        for (int i = 0; i < N; ++i) u[i] = w[i];
-        f.turn(u, a, true);
-        if (g.norm) {
-          f.load(v, xr + at, on && !value);
-          float ss = 0.0f;
+            for (int i = 0; i < N; ++i) {
+              v[k][i] *= r;
+              const float mine = on && !value ? u[i] * v[k][i] : 0.0f;
+              dgain[0][i] += query ? mine : 0.0f;
+              dgain[1][i] += query ? 0.0f : mine;
+              u[i] *= gain[i];
+              dot = fmaf(u[i], v[k][i], dot);
+            }
+            dot = group_sum<L>(dot) * inv;
 #pragma unroll
-          for (int i = 0; i < N; ++i) ss = fmaf(v[i], v[i], ss);
-          const float r = 1.0f / sqrtf(group_sum<L>(ss) * inv + g.eps);
-          float dot = 0.0f;
-#pragma unroll
-          for (int i = 0; i < N; ++i) {
-            v[i] *= r;
-            const float mine = on && !value ? u[i] * v[i] : 0.0f;
-            dgain[0][i] += h < g.heads ? mine : 0.0f;
-            dgain[1][i] += h < g.heads ? 0.0f : mine;
-            u[i] *= h < g.heads ? gain[0][i] : gain[1][i];
-            dot = fmaf(u[i], v[i], dot);
+            for (int i = 0; i < N; ++i) u[i] = (u[i] - v[k][i] * dot) * r;
           }
-          dot = group_sum<L>(dot) * inv;
 #pragma unroll
-          for (int i = 0; i < N; ++i) u[i] = (u[i] - v[i] * dot) * r;
+          for (int i = 0; i < N; ++i) u[i] = value ? w[k][i] : u[i];
         }
-#pragma unroll
-        for (int i = 0; i < N; ++i) u[i] = value ? w[i] : u[i];
+        if (on) f.store(u, outr + static_cast<int64_t>(h) * g.dh);
       }
-      if (on) f.store(u, outr + at);
     }
     t += rows_at_once;
     while (t >= g.T) {   // at most rows_at_once times
@@ -278,20 +321,31 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const float *x, const 
   }
 }
 
-// dgamma[c] = sum over workgroups, in a fixed order, in float64: sixteen columns to a workgroup, sixteen threads to a column
-__global__ __launch_bounds__(kThreads) void rotate_fold_kernel(const float *__restrict__ part, int parts, int dh, float *__restrict__ dgq,
-                                                               float *__restrict__ dgk) {
-  __shared__ double sums[16][16];
+// dgamma[c] = sum over workgroups, in a fixed order, in float64: sixteen columns to a workgroup, 64 threads to a column, each
+// with eight loads in flight.
+constexpr int kFoldThreads = 1024, kFoldSlices = kFoldThreads / 16;
+__global__ __launch_bounds__(kFoldThreads) void rotate_fold_kernel(const float *__restrict__ part, int parts, int dh, float *__restrict__ dgq,
+                                                                   float *__restrict__ dgk) {
+  __shared__ double sums[kFoldSlices][16];
   const int c = static_cast<int>(blockIdx.x) * 16 + static_cast<int>(threadIdx.x & 15u), slice = static_cast<int>(threadIdx.x >> 4);
+  const int cc = c < 2 * dh ? c : 2 * dh - 1;
   double s = 0.0;
-  if (c < 2 * dh)
-    for (int p = slice; p < parts; p += 16) s += static_cast<double>(part[static_cast<int64_t>(p) * 2 * dh + c]);
+  for (int p = slice; p < parts; p += 8 * kFoldSlices) {
+    float v[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) v[u] = part[static_cast<int64_t>(min(p + u * kFoldSlices, parts - 1)) * 2 * dh + cc];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) s += p + u * kFoldSlices < parts ? static_cast<double>(v[u]) : 0.0;
+  }
   sums[slice][threadIdx.x & 15u] = s;
   __syncthreads();
+  for (int half = kFoldSlices / 2; half > 0; half >>= 1) {
+    if (slice < half) sums[slice][threadIdx.x & 15u] += sums[slice + half][threadIdx.x & 15u];
+    __syncthreads();
+  }
   if (slice == 0 && c < 2 * dh) {
-    for (int k = 1; k < 16; ++k) s += sums[k][threadIdx.x & 15u];
     float *const to = c < dh ? dgq : dgk;
-    if (to) to[c < dh ? c : c - dh] = static_cast<float>(s);
+    if (to) to[c < dh ? c : c - dh] = static_cast<float>(sums[0][threadIdx.x & 15u]);
   }
 }
 
@@ -309,7 +363,9 @@ template <class F, bool BWD>
 aqt_status launch_as(const float *x, const float *y, RotateGeom g, float *out, float *part, hipStream_t st, unsigned *blocks) {
   g.per_row = 1;   // by all heads, in place too: the same lanes add up the same terms
   while (g.per_row < 64 / F::LANES && g.per_row < g.heads + 2 * g.kv_heads) g.per_row *= 2;
-  *blocks = rotate_blocks(g.M, 64 / F::LANES / g.per_row, part ? kFoldBlocks : kBlocks);
+  const int rows_at_once = 64 / F::LANES / g.per_row;
+  *blocks = rotate_blocks(g.M, rows_at_once, part ? kFoldBlocks : kBlocks);
+  g.each = cdiv(cdiv(g.M, rows_at_once), static_cast<int64_t>(*blocks) * (kThreads / 64)) * rows_at_once;
   rotate_kernel<F, BWD><<<*blocks, kThreads, 0, st>>>(x, y, g, out, part);
   AQT_HIP(hipGetLastError());
   return AQT_OK;
@@ -333,7 +389,7 @@ RotateGeom rotate_geom(int64_t B, int64_t T, const aqt_qk_norm_rotate &s, const 
   g.T = T; g.M = B * T;
   g.ld = (static_cast<int64_t>(s.heads) + 2 * static_cast<int64_t>(s.kv_heads)) * s.dh;
   g.heads = s.heads; g.kv_heads = s.kv_heads; g.dh = s.dh; g.rot = s.rot;
-  g.norm = s.norm; g.in_place = in_place; g.per_row = 1;
+  g.norm = s.norm; g.in_place = in_place; g.per_row = 1; g.each = 0;
   g.eps = s.eps; g.turns = s.turns; g.first = first;
   g.gamma[0] = s.gamma_q; g.gamma[1] = s.gamma_k;
   return g;
@@ -369,7 +425,7 @@ aqt_status launch_rotate_bwd(const float *qkv, const float *dout, int64_t B, int
   AQT_TRY((s.pairing == AQT_ROTATE_HALVES ? launch_paired<true, true>(qkv, dout, g, dqkv, part, al, st, &blocks)
                                           : launch_paired<false, true>(qkv, dout, g, dqkv, part, al, st, &blocks)));
   if (!part) return AQT_OK;
-  rotate_fold_kernel<<<static_cast<unsigned>(cdiv(2 * s.dh, 16)), kThreads, 0, st>>>(part, static_cast<int>(blocks), s.dh, dgamma_q, dgamma_k);
+  rotate_fold_kernel<<<static_cast<unsigned>(cdiv(2 * s.dh, 16)), kFoldThreads, 0, st>>>(part, static_cast<int>(blocks), s.dh, dgamma_q, dgamma_k);
   AQT_HIP(hipGetLastError());
   return AQT_OK;
 }

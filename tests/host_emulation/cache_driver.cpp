@@ -20,11 +20,11 @@ static void quantized(const float *x, int dh, int qmax, std::vector<double> &to,
   }
 }
 
-template <int L, bool VEC> static void append(unsigned grid, const float *qkv, const CacheGeom &g, int64_t T, int heads, const int32_t *count, int quads, int per, int32_t *st) {
-  run(grid, 256, 0, [&] { cache_::cache_append_kernel<L, VEC>(qkv, g, T, heads, count, quads, per, st); });
+template <int L, bool VEC> static void append(unsigned grid, const float *qkv, const CacheGeom &g, int64_t T, int heads, const int32_t *count, int run_, int per, int32_t *st) {
+  run(grid, 256, 0, [&] { cache_::cache_append_kernel<L, VEC>(qkv, g, T, heads, count, run_, per, st); });
 }
-template <int L, bool VEC> static void read_(unsigned grid, const CacheGeom &g, int64_t pend, const int32_t *count, const int64_t *first, int64_t n, int quads, int per, float *k, float *v) {
-  run(grid, 256, 0, [&] { cache_::cache_read_kernel<L, VEC>(g, pend, count, first, n, quads, per, k, v); });
+template <int L, bool VEC> static void read_(unsigned grid, const CacheGeom &g, int64_t pend, const int32_t *count, const int64_t *first, int64_t n, int run_, int per, float *k, float *v) {
+  run(grid, 256, 0, [&] { cache_::cache_read_kernel<L, VEC>(g, pend, count, first, n, run_, per, k, v); });
 }
 
 static void one(int streams, int64_t capacity, int heads, int kv, int dh, int bits, std::vector<int> steps, std::vector<std::pair<int, int>> windows, bool ragged) {
@@ -55,10 +55,10 @@ static void one(int streams, int64_t capacity, int heads, int kv, int dh, int bi
       if (streams > 2) count[2] = -1;
     }
     const int64_t most = std::min<int64_t>(T, capacity);
-    const int L = cache_::lanes_of(dh), quads = (int)cache_::quads_of(most), per = (int)cache_::blocks_of(g, most);
+    const int L = cache_::lanes_of(dh), per = (int)cache_::cut_of(g, most).blocks;
     const bool vec = dh % 4 == 0;
     auto ap = L == 4 ? (vec ? append<4, true> : append<4, false>) : L == 8 ? (vec ? append<8, true> : append<8, false>) : (vec ? append<16, true> : append<16, false>);
-    ap((unsigned)(per * streams), qkv, g, T, heads, count, quads, per, &status);
+    ap((unsigned)(per * streams), qkv, g, T, heads, count, cache_::cut_of(g, most).log2_run, per, &status);
     std::vector<int> cnt(streams);
     for (int b = 0; b < streams; ++b) {
       cnt[b] = count ? std::min(std::max(count[b], 0), T) : T;
@@ -77,9 +77,9 @@ static void one(int streams, int64_t capacity, int heads, int kv, int dh, int bi
     for (int b = 0; b < streams; ++b) first[b] = length[b] - 3;
     float *rk = (float *)malloc(streams * nr * kv * dh * 4), *rv = (float *)malloc(streams * nr * kv * dh * 4);
     memset(rk, 0xFF, streams * nr * kv * dh * 4); memset(rv, 0xFF, streams * nr * kv * dh * 4);
-    const int rper = (int)cache_::blocks_of(g, nr), rquads = (int)cache_::quads_of(nr);
+    const int rper = (int)cache_::cut_of(g, nr).blocks;
     auto rd = L == 4 ? (vec ? read_<4, true> : read_<4, false>) : L == 8 ? (vec ? read_<8, true> : read_<8, false>) : (vec ? read_<16, true> : read_<16, false>);
-    rd((unsigned)(rper * streams), g, T, count, first, nr, rquads, rper, rk, rv);
+    rd((unsigned)(rper * streams), g, T, count, first, nr, cache_::cut_of(g, nr).log2_run, rper, rk, rv);
     for (int b = 0; b < streams; ++b) for (int64_t i = 0; i < nr; ++i) {
       const int64_t p = first[b] + i, end = (int64_t)ref.k[b].size();
       for (int e = 0; e < kv * dh; ++e) {
@@ -156,6 +156,8 @@ static void one(int streams, int64_t capacity, int heads, int kv, int dh, int bi
 template <class F, bool BWD> static void turn_kernel(const float *x, const float *y, turn::RotateGeom g, float *out, float *part, int blocks) {
   g.per_row = 1;
   while (g.per_row < 64 / F::LANES && g.per_row < g.heads + 2 * g.kv_heads) g.per_row *= 2;
+  const int rows = 64 / F::LANES / g.per_row;
+  g.each = cdiv(cdiv(g.M, rows), 4 * blocks) * rows;
   run((unsigned)blocks, 256, 0, [&] { turn::rotate_kernel<F, BWD>(x, y, g, out, part); });
 }
 template <bool HALVES, bool BWD> static void turn_paired(const float *x, const float *y, const turn::RotateGeom &g, float *out, float *part, bool pieces, int blocks) {
@@ -191,7 +193,7 @@ static void rotate_case(int64_t B, int64_t T, int heads, int kv, int dh, int rot
       if (memcmp(io, out, n * 4)) complain("in place");
       free(io);
     }
-    run((unsigned)((2 * dh + 15) / 16), 256, 0, [&] { turn::rotate_fold_kernel(part, blocks, dh, dgq, dgk); });
+    run((unsigned)((2 * dh + 15) / 16), turn::kFoldThreads, 0, [&] { turn::rotate_fold_kernel(part, blocks, dh, dgq, dgk); });
     double worst = 0, worst_dx = 0, worst_g = 0;
     std::vector<double> rq(dh, 0.0), rk(dh, 0.0), mq(dh, 1e-30), mk(dh, 1e-30);
     for (int64_t m = 0; m < B * T; ++m) for (int h = 0; h < heads + 2 * kv; ++h) {

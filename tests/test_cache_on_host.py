@@ -19,6 +19,7 @@ def spliced():
     helpers = "namespace aqt {\n" + "".join(rule_line + "\n" for rule_line in (
         "inline int qmax_of(int bits) { return (1 << (bits - 1)) - 1; }", "inline bool packed4(int bits_w) { return bits_w <= 4; }")) + "}\n"
     shim = ('#define AQT_ON_HOST 1\n#include "vectors_on_host.h"\n#include "aqt.h"\n'
+            "inline float __builtin_amdgcn_rsqf(float x) { return 1.0f / sqrtf(x); }\n"
             "inline float __shfl(float v, int lane) { return lane_value(v, (unsigned)lane); }\n")
     return (shim + helpers + layout + read("quant_code.h") + kernels("cache.hip", "cache_", "}  // namespace\n\nbool cache_shape_ok") +
             kernels("attention_cached.hip", "attend", "// Workgroups that share the tiles of 16 rows.") +
