@@ -21,9 +21,9 @@ namespace aqt {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kBlocks = 2048;       // eight workgroups to a CU: 32 wavefronts
-constexpr int kFoldBlocks = 1024;   // ... where every workgroup leaves column sums behind
-constexpr int kFwdHeads = 2, kBwdHeads = 1;   // heads of a lane whose loads are in flight together
+constexpr int kBlocks = 16384;      // one row to a wavefront up to there (128 x 512 rows of 1024 columns, forward: 113 us with 2048, 97)
+constexpr int kFoldBlocks = 1024;   // where every workgroup leaves column sums behind: what fits the chip (gradient 144 us, 152 with 4096)
+constexpr int kFwdHeads = 2, kBwdHeads = 1;   // heads of a lane whose loads are in flight together (two backward: 44 -> 52 us, fewer wavefronts fit)
 constexpr int kMaxPairs = 64;                 // of the widest head
 typedef float v4f __attribute__((ext_vector_type(4)));
 
@@ -33,7 +33,8 @@ struct RotateGeom {
   int rot;                  // columns that are rotated
   int norm, in_place;       // in place: values are where they belong already
   int per_row;              // groups of lanes that share a row: a power of two
-  int64_t each;             // rows of a wavefront's run
+  int64_t stride;           // rows that all wavefronts take at a time
+  int64_t stride_b, stride_t;   // ... in utterances and frames
   float eps;
   const double *turns;
   const int64_t *first;     // nullable: frame number of every utterance's first row
@@ -197,13 +198,13 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const float *x, const 
     for (int i = 0; i < N; ++i) dgain[w][i] = 0.0f;
   __syncthreads();
 
-  // this wavefront's run of rows
+  // All wavefronts walk the rows side by side: what is in flight at a time is one piece of memory
+  // (32 x 400 rows of 1536 columns, forward, with a run of rows to each instead: 32 us, 26.5 so).
   const int64_t wave = static_cast<int64_t>(blockIdx.x) * (kThreads / 64) + (tid >> 6);
-  const int64_t begin = wave * g.each, end = begin + g.each < g.M ? begin + g.each : g.M;
+  const int64_t begin = wave * rows_at_once, own = begin + row_of;
   const float inv = 1.0f / static_cast<float>(g.dh);
-  const int64_t own = begin + row_of;
   int64_t b, t;
-  if (g.M >> 31 == 0) {   // (a divide of 64 bits takes longer than the rest of a short call)
+  if (g.M >> 30 == 0) {   // (a divide of 64 bits takes longer than the rest of a short call)
     const uint32_t q = static_cast<uint32_t>(own) / static_cast<uint32_t>(g.T);
     b = q;
     t = static_cast<uint32_t>(own) - q * static_cast<uint32_t>(g.T);
@@ -211,9 +212,9 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const float *x, const 
     b = own / g.T;
     t = own - b * g.T;
   }
-  for (int64_t m0 = begin; m0 < end; m0 += rows_at_once) {
+  for (int64_t m0 = begin; m0 < g.M; m0 += g.stride) {
     const int64_t m = m0 + row_of;
-    const bool row_ok = m < end;
+    const bool row_ok = m < g.M;
     const double frame = row_ok ? static_cast<double>((g.first ? g.first[b] : 0) + t) : 0.0;
     const float *const xr = x + m * g.ld, *const yr = BWD ? y + m * g.ld : nullptr;
     float *const outr = out + m * g.ld;
@@ -292,8 +293,9 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const float *x, const 
         if (on) f.store(u, outr + static_cast<int64_t>(h) * g.dh);
       }
     }
-    t += rows_at_once;
-    while (t >= g.T) {   // at most rows_at_once times
+    b += g.stride_b;
+    t += g.stride_t;
+    if (t >= g.T) {
       t -= g.T;
       ++b;
     }
@@ -365,7 +367,9 @@ aqt_status launch_as(const float *x, const float *y, RotateGeom g, float *out, f
   while (g.per_row < 64 / F::LANES && g.per_row < g.heads + 2 * g.kv_heads) g.per_row *= 2;
   const int rows_at_once = 64 / F::LANES / g.per_row;
   *blocks = rotate_blocks(g.M, rows_at_once, part ? kFoldBlocks : kBlocks);
-  g.each = cdiv(cdiv(g.M, rows_at_once), static_cast<int64_t>(*blocks) * (kThreads / 64)) * rows_at_once;
+  g.stride = static_cast<int64_t>(*blocks) * (kThreads / 64) * rows_at_once;
+  g.stride_b = g.stride / g.T;
+  g.stride_t = g.stride % g.T;
   rotate_kernel<F, BWD><<<*blocks, kThreads, 0, st>>>(x, y, g, out, part);
   AQT_HIP(hipGetLastError());
   return AQT_OK;
@@ -389,7 +393,7 @@ RotateGeom rotate_geom(int64_t B, int64_t T, const aqt_qk_norm_rotate &s, const 
   g.T = T; g.M = B * T;
   g.ld = (static_cast<int64_t>(s.heads) + 2 * static_cast<int64_t>(s.kv_heads)) * s.dh;
   g.heads = s.heads; g.kv_heads = s.kv_heads; g.dh = s.dh; g.rot = s.rot;
-  g.norm = s.norm; g.in_place = in_place; g.per_row = 1; g.each = 0;
+  g.norm = s.norm; g.in_place = in_place; g.per_row = 1; g.stride = g.stride_b = g.stride_t = 0;
   g.eps = s.eps; g.turns = s.turns; g.first = first;
   g.gamma[0] = s.gamma_q; g.gamma[1] = s.gamma_k;
   return g;

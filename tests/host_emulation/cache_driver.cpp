@@ -157,7 +157,9 @@ template <class F, bool BWD> static void turn_kernel(const float *x, const float
   g.per_row = 1;
   while (g.per_row < 64 / F::LANES && g.per_row < g.heads + 2 * g.kv_heads) g.per_row *= 2;
   const int rows = 64 / F::LANES / g.per_row;
-  g.each = cdiv(cdiv(g.M, rows), 4 * blocks) * rows;
+  g.stride = 4 * blocks * rows;
+  g.stride_b = g.stride / g.T;
+  g.stride_t = g.stride % g.T;
   run((unsigned)blocks, 256, 0, [&] { turn::rotate_kernel<F, BWD>(x, y, g, out, part); });
 }
 template <bool HALVES, bool BWD> static void turn_paired(const float *x, const float *y, const turn::RotateGeom &g, float *out, float *part, bool pieces, int blocks) {
