@@ -1,0 +1,79 @@
+// What the kernels of the attention over the cache share (attention_cached.hip, attention_cached_few.hip).
+#pragma once
+#include "cache.h"
+
+namespace aqt {
+
+struct CachedGeom {
+  int64_t T, ld;            // new rows per stream, columns of a row
+  int heads, group;         // query heads, and how many of them share a key / value head
+  int row_tiles, splits;
+  int64_t left, right;      // negative: no limit
+  float scale_log2e;
+};
+// Wavefronts per SIMD that the kernel's registers are shared out to, without spills (dt: blocks of 16 head columns, r: rows).
+constexpr int few_waves(int dt, bool packed, int r) { return dt == 8 ? (packed && r < 4 ? 3 : 2) : r == 4 && !packed ? 3 : 4; }
+constexpr int kFewRows = 4;   // rows per key / value head and stream up to which attention_cached_few.hip takes the call
+// part: the splits' rows, [rows][columns], then maxima and sums [rows] each, one after the other (nullptr: straight to ctx)
+aqt_status launch_attention_cached_few(const float *qkv, const CacheGeom &g, const CachedGeom &a, const int32_t *count, float *ctx,
+                                       uint32_t *absmax, float *part, hipStream_t st);
+
+namespace {
+
+constexpr int kThreads = 256, kWaves = 4;
+constexpr float kLowest = -3.402823466e38f;
+constexpr float kDigits = 8355584.0f;     // 0x7F7F00: balanced digits of at most 0x7F7F7F, a rounding of the quotient allowed for
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef int v4i __attribute__((ext_vector_type(4)));
+typedef int v2i __attribute__((ext_vector_type(2)));
+
+// Four integers of 24 bits, the digits of one weight each to a dword: d[0] the highest.
+__device__ __forceinline__ void digits4(const int (&n)[4], int &d0, int &d1, int &d2) {
+  uint32_t u[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) u[i] = (static_cast<uint32_t>(n[i]) + 0x00808080u) ^ 0x00808080u;
+  const uint32_t ab = __builtin_amdgcn_perm(u[1], u[0], 0x05010400u), cd = __builtin_amdgcn_perm(u[3], u[2], 0x05010400u);   // a0 b0 a1 b1
+  const uint32_t at = __builtin_amdgcn_perm(u[1], u[0], 0x0C0C0602u), ct = __builtin_amdgcn_perm(u[3], u[2], 0x0C0C0602u);   // a2 b2
+  d2 = static_cast<int>(__builtin_amdgcn_perm(cd, ab, 0x05040100u));
+  d1 = static_cast<int>(__builtin_amdgcn_perm(cd, ab, 0x07060302u));
+  d0 = static_cast<int>(__builtin_amdgcn_perm(ct, at, 0x05040100u));
+}
+
+__device__ __forceinline__ v4i mfma_i8(v4i a, v4i b, v4i c) { return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0); }
+
+// The three digits' sums as one number, 256^2 a + 256 b + c.
+__device__ __forceinline__ float joined(int a, int b, int c) {
+  return fmaf(static_cast<float>(a), 65536.0f, static_cast<float>(b * 256 + c));
+}
+
+__device__ __forceinline__ float max_of_groups(float v) {   // over the four lanes of a row
+  v = fmaxf(v, __shfl_xor(v, 16, 64));
+  return fmaxf(v, __shfl_xor(v, 32, 64));
+}
+
+// Four columns of a row of ctx.
+__device__ __forceinline__ uint32_t put_ctx(float *to, int col, int dh, v4f v) {
+  uint32_t amax = 0u;
+  const float x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (col + e < dh) {
+      to[col + e] = x[e];
+      amax = max(amax, __float_as_uint(x[e]) & 0x7FFFFFFFu);
+    }
+  return amax;
+}
+__device__ __forceinline__ void put_absmax(uint32_t *absmax, uint32_t amax) {   // the word only grows: a stale read can only cost an atomic
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) amax = max(amax, static_cast<uint32_t>(__shfl_xor(static_cast<int>(amax), off, 64)));
+  if ((threadIdx.x & 63u) == 0 && amax > *reinterpret_cast<volatile uint32_t *>(absmax)) atomicMax(absmax, amax);
+}
+
+// What a workgroup leaves where several share the tiles: [rows][columns], then the rows' maxima and sums.
+template <int ROWS, int COLS>
+struct Partial {
+  static constexpr int kMax = ROWS * COLS, kSum = kMax + ROWS, kFloats = (kSum + ROWS + 3) / 4 * 4;
+};
+
+}  // namespace
+}  // namespace aqt

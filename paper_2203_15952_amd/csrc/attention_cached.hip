@@ -15,74 +15,13 @@
 //   a lane (row lr = lane % 16, g = lane / 16) then holds the scores of the frames 16 t + 4 g + r of its row
 //   O^T (dh x 16 rows) += V^T P^T         B operand: the digits of the lane's own probabilities, where they stand; A operand:
 //                                         value rows, whose frames the cache keeps in that order
-#include "cache.h"
+#include "attention_cached.h"
 
 namespace aqt {
 namespace {
 
-constexpr int kThreads = 256, kWaves = 4;
 constexpr int kRows = 16;                 // rows of a workgroup
-constexpr float kLowest = -3.402823466e38f;
-constexpr float kDigits = 8355584.0f;     // 0x7F7F00: balanced digits of at most 0x7F7F7F, a rounding of the quotient allowed for
-typedef float v4f __attribute__((ext_vector_type(4)));
-typedef int v4i __attribute__((ext_vector_type(4)));
-typedef int v2i __attribute__((ext_vector_type(2)));
-
-struct CachedGeom {
-  int64_t T, ld;            // new rows per stream, columns of a row
-  int heads, group;         // query heads, and how many of them share a key / value head
-  int row_tiles, splits;
-  int64_t left, right;      // negative: no limit
-  float scale_log2e;
-};
-
-// Four integers of 24 bits, the digits of one weight each to a dword: d[0] the highest.
-__device__ __forceinline__ void digits4(const int (&n)[4], int &d0, int &d1, int &d2) {
-  uint32_t u[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) u[i] = (static_cast<uint32_t>(n[i]) + 0x00808080u) ^ 0x00808080u;
-  const uint32_t ab = __builtin_amdgcn_perm(u[1], u[0], 0x05010400u), cd = __builtin_amdgcn_perm(u[3], u[2], 0x05010400u);   // a0 b0 a1 b1
-  const uint32_t at = __builtin_amdgcn_perm(u[1], u[0], 0x0C0C0602u), ct = __builtin_amdgcn_perm(u[3], u[2], 0x0C0C0602u);   // a2 b2
-  d2 = static_cast<int>(__builtin_amdgcn_perm(cd, ab, 0x05040100u));
-  d1 = static_cast<int>(__builtin_amdgcn_perm(cd, ab, 0x07060302u));
-  d0 = static_cast<int>(__builtin_amdgcn_perm(ct, at, 0x05040100u));
-}
-
-__device__ __forceinline__ v4i mfma_i8(v4i a, v4i b, v4i c) { return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0); }
-
-// The three digits' sums as one number, 256^2 a + 256 b + c.
-__device__ __forceinline__ float joined(int a, int b, int c) {
-  return fmaf(static_cast<float>(a), 65536.0f, static_cast<float>(b * 256 + c));
-}
-
-__device__ __forceinline__ float max_of_groups(float v) {   // over the four lanes of a row
-  v = fmaxf(v, __shfl_xor(v, 16, 64));
-  return fmaxf(v, __shfl_xor(v, 32, 64));
-}
-
-// What a workgroup leaves: the rows' running maxima and sums, and their sums of values.
-template <int COLS>
-struct Partial {
-  static constexpr int kMax = 0, kSum = kRows, kOut = 2 * kRows, kFloats = kOut + kRows * COLS;
-};
-
-// The rows of a workgroup or of its joined parts leave as ctx; thread (row = tid / 16, columns 4 (tid % 16) + 64 k).
-__device__ __forceinline__ uint32_t put_ctx(float *to, int col, int dh, v4f v) {
-  uint32_t amax = 0u;
-  const float x[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-  for (int e = 0; e < 4; ++e)
-    if (col + e < dh) {
-      to[col + e] = x[e];
-      amax = max(amax, __float_as_uint(x[e]) & 0x7FFFFFFFu);
-    }
-  return amax;
-}
-__device__ __forceinline__ void put_absmax(uint32_t *absmax, uint32_t amax) {   // the word only grows: a stale read can only cost an atomic
-#pragma unroll
-  for (int off = 32; off > 0; off >>= 1) amax = max(amax, static_cast<uint32_t>(__shfl_xor(static_cast<int>(amax), off, 64)));
-  if ((threadIdx.x & 63u) == 0 && amax > *reinterpret_cast<volatile uint32_t *>(absmax)) atomicMax(absmax, amax);
-}
+constexpr int64_t kWorkgroups = 2048;
 
 // DT: blocks of 16 head columns that a workgroup holds (2, 4 or 8)
 template <int DT, bool PACKED>
@@ -292,7 +231,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_cached_kernel(const flo
   const int out_row = rt * kRows + orow, t = out_row / a.group;
   const bool store = t < n;
   float *const to = ctx + ((b * a.T + t) * a.heads + h * a.group + out_row % a.group) * g.dh;
-  float *const left = part ? part + static_cast<int64_t>(blockIdx.x) * Partial<COLS>::kFloats : nullptr;
+  float *const left = part ? part + static_cast<int64_t>(blockIdx.x) * Partial<kRows, COLS>::kFloats : nullptr;
   const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;   // nothing seen: zeros
   uint32_t amax = 0u;
 #pragma unroll
@@ -305,7 +244,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_cached_kernel(const flo
       for (int e = 0; e < 4; ++e) v[e] = fmaf(x[e], weight[w], v[e]);
     }
     if (left) {
-      *reinterpret_cast<v4f *>(left + Partial<COLS>::kOut + orow * COLS + c) = v;
+      *reinterpret_cast<v4f *>(left + orow * COLS + c) = v;
     } else if (store) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[e] *= inv;
@@ -314,60 +253,92 @@ __global__ __launch_bounds__(kThreads, 2) void attention_cached_kernel(const flo
   }
   if (left) {
     if ((tid & 15) == 0) {
-      left[Partial<COLS>::kMax + orow] = top;
-      left[Partial<COLS>::kSum + orow] = sum;
+      left[Partial<kRows, COLS>::kMax + orow] = top;
+      left[Partial<kRows, COLS>::kSum + orow] = sum;
     }
   } else if (absmax) {
     put_absmax(absmax, amax);
   }
 }
 
-// The splits' parts of 16 rows, in their order.
-template <int COLS>
+// The splits' parts of a workgroup's rows.  Threads in as many slices as there are for the rows' columns, four columns each; a
+// slice takes every so many-th split, and the slices are joined in their order.
+template <int ROWS, int COLS>
 __global__ __launch_bounds__(kThreads) void attention_cached_join_kernel(const float *__restrict__ part, CacheGeom g, CachedGeom a,
                                                                          const int32_t *__restrict__ count, float *__restrict__ ctx,
                                                                          uint32_t *__restrict__ absmax) {
-  constexpr int F = Partial<COLS>::kFloats;
-  const int tid = static_cast<int>(threadIdx.x), orow = tid >> 4;
+  using P = Partial<ROWS, COLS>;
+  constexpr int QUADS = ROWS * COLS / 4, PER = QUADS > kThreads ? QUADS / kThreads : 1, SLICES = QUADS > kThreads ? 1 : kThreads / QUADS;
+  constexpr int N = SLICES == 1 ? 1 : SLICES;
+  __shared__ __attribute__((aligned(16))) float so[N][N == 1 ? 4 : ROWS * COLS];
+  __shared__ float sm[N][ROWS], sl[N][ROWS];
+  const int tid = static_cast<int>(threadIdx.x), slice = SLICES == 1 ? 0 : tid / QUADS;
   int64_t id = blockIdx.x;
-  const float *const from = part + id * a.splits * F;
+  const float *const from = part + id * a.splits * P::kFloats;
   const int rt = static_cast<int>(id % a.row_tiles);
   id /= a.row_tiles;
   const int h = static_cast<int>(id % g.kv_heads);
   const int64_t b = id / g.kv_heads;
   const StreamFrames f = stream_frames(g, count, a.T, b);
   const int n = static_cast<int>(f.end - f.length);
-  if (rt * kRows / a.group >= n) return;   // its parts were not written
-  const int out_row = rt * kRows + orow, t = out_row / a.group;
-  float top = kLowest, sum = 0.0f;
-  for (int s = 0; s < a.splits; ++s) top = fmaxf(top, from[static_cast<int64_t>(s) * F + Partial<COLS>::kMax + orow]);
-  constexpr int N = (COLS + 63) / 64;
-  v4f v[N];
+  uint32_t amax = 0u;                     // (parts of frames that the stream did not bring were not written, and are not stored)
 #pragma unroll
-  for (int k = 0; k < N; ++k) v[k] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-  const int c0 = 4 * (tid & 15);
-#pragma unroll 4
-  for (int s = 0; s < a.splits; ++s) {
-    const float *const p = from + static_cast<int64_t>(s) * F;
-    const float w = __builtin_amdgcn_exp2f(p[Partial<COLS>::kMax + orow] - top);
-    sum = fmaf(p[Partial<COLS>::kSum + orow], w, sum);
+  for (int k = 0; k < PER; ++k) {
+    const int quad = SLICES == 1 ? k * kThreads + tid : tid % QUADS, row = quad / (COLS / 4), c = 4 * (quad % (COLS / 4));
+    float top = kLowest, sum = 0.0f;
+    v4f v = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int s0 = slice; s0 < a.splits; s0 += 4 * SLICES) {   // four parts' loads in flight
+      float m[4], l[4];
+      v4f x[4];
 #pragma unroll
-    for (int k = 0; k < N; ++k) {
-      const int c = c0 + 64 * k < COLS ? c0 + 64 * k : 0;
-      const v4f x = *reinterpret_cast<const v4f *>(p + Partial<COLS>::kOut + orow * COLS + c);
+      for (int u = 0; u < 4; ++u) {
+        const int s = s0 + u * SLICES;
+        const float *const p = from + static_cast<int64_t>(s < a.splits ? s : slice) * P::kFloats;
+        m[u] = s < a.splits ? p[P::kMax + row] : kLowest;
+        l[u] = s < a.splits ? p[P::kSum + row] : 0.0f;
+        x[u] = *reinterpret_cast<const v4f *>(p + row * COLS + c);
+      }
+      const float next = fmaxf(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])), top), alpha = __builtin_amdgcn_exp2f(top - next);
+      top = next;
+      sum *= alpha;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[k][e] = fmaf(x[e], w, v[k][e]);
+      for (int e = 0; e < 4; ++e) v[e] *= alpha;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const float w = s0 + u * SLICES < a.splits ? __builtin_amdgcn_exp2f(m[u] - top) : 0.0f;
+        sum = fmaf(l[u], w, sum);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = s0 + u * SLICES < a.splits ? fmaf(x[u][e], w, v[e]) : v[e];
+      }
     }
-  }
-  const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
-  uint32_t amax = 0u;
-  if (t < n) {
-    float *const to = ctx + ((b * a.T + t) * a.heads + h * a.group + out_row % a.group) * g.dh;
+    if (SLICES > 1) {
+      *reinterpret_cast<v4f *>(&so[slice][row * COLS + c]) = v;
+      if (c == 0) {
+        sm[slice][row] = top;
+        sl[slice][row] = sum;
+      }
+      __syncthreads();
+      if (slice == 0) {
 #pragma unroll
-    for (int k = 0; k < N; ++k) {
+        for (int s = 0; s < SLICES; ++s) top = fmaxf(top, sm[s][row]);
+        sum = 0.0f;
+        v = v4f{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-      for (int e = 0; e < 4; ++e) v[k][e] *= inv;
-      if (c0 + 64 * k < COLS) amax = max(amax, put_ctx(to, c0 + 64 * k, g.dh, v[k]));
+        for (int s = 0; s < SLICES; ++s) {
+          const float w = __builtin_amdgcn_exp2f(sm[s][row] - top);
+          sum = fmaf(sl[s][row], w, sum);
+          const v4f x = *reinterpret_cast<const v4f *>(&so[s][row * COLS + c]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = fmaf(x[e], w, v[e]);
+        }
+      }
+    }
+    const int out_row = rt * ROWS + row, t = out_row / a.group;
+    if (slice == 0 && t < n) {
+      const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] *= inv;
+      amax = max(amax, put_ctx(ctx + ((b * a.T + t) * a.heads + h * a.group + out_row % a.group) * g.dh, c, g.dh, v));
     }
   }
   if (absmax) put_absmax(absmax, amax);
@@ -379,29 +350,53 @@ __global__ void zero_word_kernel(uint32_t *p) {
 
 int cols_of(int dh) { return dh <= 32 ? 32 : dh <= 64 ? 64 : 128; }
 
-// Workgroups that share the tiles of 16 rows.  Two thousand wavefronts keep every SIMD busy with two; a split takes at least one
-// tile per wavefront.  `window`: the longest run of frames that a row tile sees.
-int splits_of(const CacheGeom &g, int64_t row_tiles, int64_t window) {
-  const int64_t groups = g.streams * g.kv_heads * row_tiles, tiles = cdiv(window, 64) + 1;
-  const int64_t want = cdiv(1024, groups), most = cdiv(tiles, kWaves);
-  const int64_t s = want < most ? want : most;
-  return static_cast<int>(s < 1 ? 1 : s);
+// How a call is cut up: rows of a workgroup (all that share a key / value head, where they are few), row tiles, and the workgroups
+// (splits) that share the tiles of a row tile: a tile for every wavefront at most.
+struct CachedCut {
+  int rows, row_tiles, splits;
+  int64_t groups;
+};
+// window: the longest run of frames that a row tile sees
+CachedCut cut_of(const CacheGeom &g, int64_t rows, int64_t window) {
+  CachedCut c;
+  c.rows = rows <= kFewRows ? (rows == 1 ? 1 : rows == 2 ? 2 : 4) : kRows;
+  c.row_tiles = static_cast<int>(cdiv(rows, c.rows));
+  c.groups = g.streams * g.kv_heads * c.row_tiles;
+  // Few rows: as many workgroups as the chip holds at a time, a wavefront of each on every SIMD; what comes behind them would form
+  // its rows' digits and request its first tile while the others are at the memory's rate (32 streams, four rows of 128 columns:
+  // 108 us with 512 workgroups, 113 with 1024, 123 with 2048).  Sixteen rows are bound by vector instructions, and a workgroup's share
+  // had better be small (8 streams of 128 rows: 76 us with 2048, 80 with 1024, 83 with 512).
+  const int64_t want = c.rows == kRows ? cdiv(kWorkgroups, c.groups) : 256 * few_waves(cols_of(g.dh) / 16, g.packed, c.rows) / c.groups;
+  const int64_t most = cdiv(cdiv(window, 64) + 1, kWaves), s = want < most ? want : most;
+  c.splits = static_cast<int>(s < 1 ? 1 : s);
+  return c;
+}
+
+size_t part_floats(const CachedCut &c, int dh) {
+  const size_t rows = static_cast<size_t>(c.rows), one = (rows * cols_of(dh) + 2 * rows + 3) / 4 * 4;   // Partial<rows, columns>
+  return c.splits == 1 ? 0 : one * c.groups * c.splits;
+}
+
+template <int ROWS>
+void launch_join(const float *part, const CacheGeom &g, const CachedGeom &a, const int32_t *count, float *ctx, uint32_t *absmax,
+                 unsigned groups, hipStream_t st) {
+  auto join = g.dh <= 32   ? attention_cached_join_kernel<ROWS, 32>
+              : g.dh <= 64 ? attention_cached_join_kernel<ROWS, 64>
+                           : attention_cached_join_kernel<ROWS, 128>;
+  join<<<groups, kThreads, 0, st>>>(part, g, a, count, ctx, absmax);
 }
 
 }  // namespace
 
 bool cached_attention_ok(const aqt_cache &c, int64_t T, int heads) {
   if (T > (int64_t(1) << 24)) return false;
-  const int64_t row_tiles = cdiv(T * (heads / c.kv_heads), kRows);
+  const int64_t rows = T * (heads / c.kv_heads), row_tiles = cdiv(rows, rows <= kFewRows ? rows : kRows);
   return row_tiles * kRows <= (int64_t(1) << 30) && row_tiles * c.kv_heads <= (int64_t(1) << 30) / c.streams;
 }
 
 size_t cached_attention_ws_bytes(const aqt_cache &c, int64_t T, int heads) {
-  const CacheGeom g = cache_geom(c);
-  const int64_t row_tiles = cdiv(T * (heads / c.kv_heads), kRows);
-  const int splits = splits_of(g, row_tiles, c.capacity);
-  const size_t floats = 2 * kRows + static_cast<size_t>(kRows) * cols_of(c.dh);
-  return splits == 1 ? 256 : align_up(static_cast<size_t>(splits) * g.streams * g.kv_heads * row_tiles * floats * sizeof(float), 256);
+  const size_t bytes = part_floats(cut_of(cache_geom(c), T * (heads / c.kv_heads), c.capacity), c.dh) * sizeof(float);
+  return bytes < 256 ? 256 : align_up(bytes, 256);
 }
 
 aqt_status launch_attention_cached(const float *qkv, int64_t T, int heads, const aqt_cache &c, const int32_t *count, int left, int right,
@@ -412,30 +407,34 @@ aqt_status launch_attention_cached(const float *qkv, int64_t T, int heads, const
   a.heads = heads;
   a.group = heads / c.kv_heads;
   a.ld = (static_cast<int64_t>(heads) + 2 * static_cast<int64_t>(c.kv_heads)) * c.dh;
-  a.row_tiles = static_cast<int>(cdiv(T * a.group, kRows));
   a.left = left;
   a.right = right;
   a.scale_log2e = static_cast<float>(1.4426950408889634 / sqrt(static_cast<double>(c.dh)));
-  // 16 rows span at most that many frames, and a window on either side of them
+  // a tile's rows span at most that many frames, and a window on either side of them
   const int64_t span = cdiv(kRows, a.group) + 1, window = left < 0 ? c.capacity : span + left + (right < 0 ? T : right);
-  a.splits = splits_of(g, a.row_tiles, window < c.capacity ? window : c.capacity);
+  const CachedCut cut = cut_of(g, T * a.group, window < c.capacity ? window : c.capacity);
+  a.row_tiles = cut.row_tiles;
+  a.splits = cut.splits;
   if (absmax) {
     zero_word_kernel<<<1, 64, 0, st>>>(absmax);
     AQT_HIP(hipGetLastError());
   }
-  const int64_t groups = g.streams * g.kv_heads * a.row_tiles;
-  float *const part = a.splits > 1 ? static_cast<float *>(ws) : nullptr;
-  auto kern = g.packed ? (c.dh <= 32   ? attention_cached_kernel<2, true>
-                          : c.dh <= 64 ? attention_cached_kernel<4, true>
-                                       : attention_cached_kernel<8, true>)
-                       : (c.dh <= 32   ? attention_cached_kernel<2, false>
-                          : c.dh <= 64 ? attention_cached_kernel<4, false>
-                                       : attention_cached_kernel<8, false>);
-  kern<<<static_cast<unsigned>(groups * a.splits), kThreads, 0, st>>>(qkv, g, a, count, ctx, absmax, part);
-  AQT_HIP(hipGetLastError());
+  float *const part = cut.splits > 1 ? static_cast<float *>(ws) : nullptr;
+  if (cut.rows != kRows) {
+    AQT_TRY(launch_attention_cached_few(qkv, g, a, count, ctx, absmax, part, st));
+  } else {
+    auto kern = g.packed ? (c.dh <= 32   ? attention_cached_kernel<2, true>
+                            : c.dh <= 64 ? attention_cached_kernel<4, true>
+                                         : attention_cached_kernel<8, true>)
+                         : (c.dh <= 32   ? attention_cached_kernel<2, false>
+                            : c.dh <= 64 ? attention_cached_kernel<4, false>
+                                         : attention_cached_kernel<8, false>);
+    kern<<<static_cast<unsigned>(cut.groups * cut.splits), kThreads, 0, st>>>(qkv, g, a, count, ctx, absmax, part);
+    AQT_HIP(hipGetLastError());
+  }
   if (!part) return AQT_OK;
-  auto join = c.dh <= 32 ? attention_cached_join_kernel<32> : c.dh <= 64 ? attention_cached_join_kernel<64> : attention_cached_join_kernel<128>;
-  join<<<static_cast<unsigned>(groups), kThreads, 0, st>>>(part, g, a, count, ctx, absmax);
+  auto join = cut.rows == 1 ? launch_join<1> : cut.rows == 2 ? launch_join<2> : cut.rows == 4 ? launch_join<4> : launch_join<kRows>;
+  join(part, g, a, count, ctx, absmax, static_cast<unsigned>(cut.groups), st);
   AQT_HIP(hipGetLastError());
   return AQT_OK;
 }

@@ -1,0 +1,318 @@
+// Attention over the quantized cache where at most four rows (new frame, query head) share a key / value head: single frames, with
+// or without grouped heads.  The digits and products of attention_cached.hip; there a lane holds sixteen scores of one of
+// sixteen rows, which for one row is sixteen times the vector work that there is (16 streams, one frame over 4000 to 16000 frames,
+// int8: 41 us, 31 here; 32 streams, four rows, heads of 128, int4: 169 us, 109 here; reading the codes takes 23 and 88).  Here a lane holds one frame's score for
+// each row, and one column of the result:
+//   S (rows x 64 frames) = q K^T   A operand: the rows, repeated in each group of four; B operand: 16 frames at a time.  All four groups
+//                                  of lanes then hold the scores of all 16; group g keeps those of the g-th 16
+//   O (rows x dh) = P V            A operand: the probabilities' digits, through LDS (a byte per digit); B operand: value rows.  Again
+//                                  every group holds all of 16 columns, and group g keeps the g-th 16
+// The probabilities' digits are relative to exp2(largest score - running maximum) times the tile's largest value scale: a bound of
+// the tile's largest weight that takes one maximum over the wavefront per row and tile.
+#include "attention_cached.h"
+
+namespace aqt {
+namespace {
+
+// The largest of a wavefront's 64 values, in every lane.
+__device__ __forceinline__ float wave_max(float v) {
+  auto step = [&](int w) { v = fmaxf(v, __uint_as_float(static_cast<uint32_t>(w))); };
+  const auto bits = [&] { return static_cast<int>(__float_as_uint(v)); };
+  step(__builtin_amdgcn_update_dpp(bits(), bits(), 0x111, 0xF, 0xF, false));   // row_shr:1, 2, 4, 8: a row's last lane has its maximum
+  step(__builtin_amdgcn_update_dpp(bits(), bits(), 0x112, 0xF, 0xF, false));
+  step(__builtin_amdgcn_update_dpp(bits(), bits(), 0x114, 0xF, 0xF, false));
+  step(__builtin_amdgcn_update_dpp(bits(), bits(), 0x118, 0xF, 0xF, false));
+  step(__builtin_amdgcn_update_dpp(bits(), bits(), 0x142, 0xF, 0xF, false));   // row_bcast:15, 31
+  step(__builtin_amdgcn_update_dpp(bits(), bits(), 0x143, 0xF, 0xF, false));
+  return __uint_as_float(static_cast<uint32_t>(__builtin_amdgcn_readlane(bits(), 63)));
+}
+__device__ __forceinline__ float of_lane(float v, int lane) {
+  return __uint_as_float(static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(__float_as_uint(v)), lane)));
+}
+// The group's own of four.
+__device__ __forceinline__ int of_group(int a, int b, int c, int d, bool odd, bool upper) {
+  const int x = odd ? b : a, y = odd ? d : c;
+  return upper ? y : x;
+}
+
+// DT: blocks of 16 head columns (2, 4 or 8); R: rows (1, 2 or 4)
+template <int DT, bool PACKED, int R>
+__global__ __launch_bounds__(kThreads, few_waves(DT, PACKED, R)) void attention_cached_few_kernel(const float *__restrict__ qkv, CacheGeom g, CachedGeom a,
+                                                                           const int32_t *__restrict__ count, float *__restrict__ ctx,
+                                                                           uint32_t *__restrict__ absmax, float *__restrict__ part) {
+  constexpr int KS = DT == 8 ? 2 : 1, COLS = 16 * DT, HALVES = DT == 8 ? 2 : 1, BLOCKS = DT < 4 ? DT : 4;   // HALVES of 64 columns
+  using P = Partial<R, COLS>;
+  __shared__ __attribute__((aligned(16))) uint8_t digits[kWaves][3][R][64];
+  __shared__ float so[kWaves][R][COLS], sm[kWaves][R], sl[kWaves][R];
+  const int tid = static_cast<int>(threadIdx.x), lane = tid & 63, lr = lane & 15, lg = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const bool odd = lg & 1, upper = lg >> 1;
+  const int split = static_cast<int>(blockIdx.x) % a.splits, bh = static_cast<int>(blockIdx.x) / a.splits;
+  const int h = bh % g.kv_heads;
+  const int64_t b = bh / g.kv_heads;
+  const StreamFrames f = stream_frames(g, count, a.T, b);
+  const int n = static_cast<int>(f.end - f.length);
+  if (n == 0) return;
+  const int rows = min(static_cast<int>(a.T) * a.group, R);
+
+  // the frames that the rows see, counted from the first tile
+  auto from = [&](int t) { const int64_t x = f.length + t - a.left; return a.left < 0 || x < f.oldest ? f.oldest : x; };
+  auto upto = [&](int t) { const int64_t x = f.length + t + a.right; return a.right < 0 || x > f.end - 1 ? f.end - 1 : x; };
+  auto frame_of = [&](int row) { return min(min(row, rows - 1) / a.group, n - 1); };   // rows behind the last repeat it
+  const int64_t first = from(0), last = upto(n - 1), tile0 = first >> 6, base = tile0 * 64;
+  const int tiles = last < first ? 0 : static_cast<int>((last >> 6) - tile0) + 1;
+  int lo[R], hi[R];
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    lo[r] = static_cast<int>(from(frame_of(r)) - base);
+    hi[r] = static_cast<int>(upto(frame_of(r)) - base);
+  }
+
+  // the rows' digits: row lr % 4 of R, 16 columns per lane and step
+  v4i q[KS][3];
+  float row_scale[R];
+  {
+    const int own = min(lr & 3, R - 1), t = frame_of(own);
+    const float *const src = qkv + (b * a.T + t) * a.ld + (static_cast<int64_t>(h) * a.group + min(own, rows - 1) % a.group) * g.dh;
+    float x[KS][16];
+    uint32_t m = 0u;
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int c = 64 * k + 16 * lg + i;
+        x[k][i] = src[min(c, g.dh - 1)];
+        x[k][i] = c < g.dh ? x[k][i] : 0.0f;
+        m = max(m, __float_as_uint(x[k][i]) & 0x7FFFFFFFu);
+      }
+    m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 16, 64)));
+    m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 32, 64)));
+    const float top = __uint_as_float(m);    // a NaN or an infinity makes the row's scores NaN
+    const float to = kDigits / fmaxf(top, 0x1p-100f);
+    const float unit = (m > 0x7F800000u ? top : fmaxf(top, 0x1p-100f)) * (1.0f / kDigits) * a.scale_log2e * (PACKED ? 0.0625f : 1.0f);
+#pragma unroll
+    for (int r = 0; r < R; ++r) row_scale[r] = of_lane(unit, r);
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        int nn[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) nn[i] = static_cast<int>(rintf(x[k][4 * w + i] * to));
+        int d0, d1, d2;
+        digits4(nn, d0, d1, d2);
+        q[k][0][w] = d0;
+        q[k][1][w] = d1;
+        q[k][2][w] = d2;
+      }
+  }
+
+  const uint8_t *const head = g.data + (b * g.kv_heads + h) * g.tiles * static_cast<int64_t>(g.tile_bytes);
+  const int step = a.splits * kWaves, slot_step = step % g.tiles;
+  float m[R], l[R], o[HALVES][R];            // o: column 64 half + lane
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    m[r] = kLowest;
+    l[r] = 0.0f;
+#pragma unroll
+    for (int k = 0; k < HALVES; ++k) o[k][r] = 0.0f;
+  }
+  uint8_t *const put = &digits[wave][0][0][frame_slot(lane)];
+  const uint8_t *const take = &digits[wave][0][min(lr & 3, R - 1)][16 * lg];
+  // A tile's keys, values and scales are requested where the tile before has given up their registers: the keys' trip from memory
+  // passes under the rest of that tile, the values' under this one's scores (32 streams, four rows, int4: 132 us with all loads at the head of a tile, 118 so).
+  constexpr int KEYS = PACKED ? 2 : 4, VALUES = PACKED ? DT / 2 : DT;
+  typedef int key_piece __attribute__((ext_vector_type(KEYS)));
+  key_piece keys[4][KS];
+  v4i values[VALUES];
+  float ks, vs_next;
+  auto load_keys = [&](const uint8_t *tile) {
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {   // sixteen columns to a lane; one beyond the row meets digits of zero
+        const int at = (64 * k + 16 * lg) * KEYS / 4;
+        keys[t][k] = *reinterpret_cast<const key_piece *>(tile + (16 * t + lr) * g.key_row + (at < g.key_row ? at : 0));
+      }
+    ks = reinterpret_cast<const float *>(tile + cache_scales(g))[lane];
+  };
+  auto load_values = [&](const uint8_t *tile) {
+#pragma unroll
+    for (int d = 0; d < VALUES; ++d) {
+      const int at = 16 * d + lr;      // columns beyond the head are not stored
+      values[d] = *reinterpret_cast<const v4i *>(tile + cache_values(g) + (at < g.value_rows ? at : lr) * 64 + 16 * lg);
+    }
+    vs_next = reinterpret_cast<const float *>(tile + cache_scales(g))[64 + lane];
+  };
+  int i = split * kWaves + wave;
+  int slot = tile_slot(tile0 + i, g.tiles);
+  if (i < tiles) {
+    const uint8_t *const tile = head + static_cast<int64_t>(slot) * g.tile_bytes;
+    load_keys(tile);
+    load_values(tile);
+  }
+  for (; i < tiles; i += step) {
+    if (i + step < tiles) {   // otherwise this tile's once more: never another's memory
+      slot += slot_step;
+      slot = slot >= g.tiles ? slot - g.tiles : slot;
+    }
+    const uint8_t *const next = head + static_cast<int64_t>(slot) * g.tile_bytes;
+    float vs = vs_next;
+    const float ks_now = ks;
+    v4i c[4][3];
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {
+        v4i w;
+        if constexpr (PACKED) {
+          const uint32_t x = static_cast<uint32_t>(keys[t][k][0]), y = static_cast<uint32_t>(keys[t][k][1]);
+          w = v4i{static_cast<int>(x << 4 & 0xF0F0F0F0u), static_cast<int>(y << 4 & 0xF0F0F0F0u), static_cast<int>(x & 0xF0F0F0F0u),
+                  static_cast<int>(y & 0xF0F0F0F0u)};
+        } else {
+          w = keys[t][k];
+        }
+#pragma unroll
+        for (int d = 0; d < 3; ++d) c[t][d] = mfma_i8(q[k][d], w, k == 0 ? v4i{0, 0, 0, 0} : c[t][d]);
+      }
+    load_keys(next);
+    // the lane's frame: window (what it hides, and what is no frame of the stream's, may hold anything)
+    const int j0 = 64 * i, j = j0 + lane;
+    bool whole = true;
+#pragma unroll
+    for (int r = 0; r < R; ++r) whole = whole && j0 >= lo[r] && j0 + 63 <= hi[r];
+    float s[R];
+    bool see[R], any = false;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      int d[3];
+#pragma unroll
+      for (int e = 0; e < 3; ++e) d[e] = of_group(c[0][e][r], c[1][e][r], c[2][e][r], c[3][e][r], odd, upper);
+      see[r] = whole || (j >= lo[r] && j <= hi[r]);
+      any = any || see[r];
+      s[r] = joined(d[0], d[1], d[2]) * (row_scale[r] * ks_now);
+    }
+    vs = any ? vs : 0.0f;
+    const float vs_top = wave_max(vs);
+    float alpha[R], unit[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      const float mx = wave_max(see[r] ? s[r] : kLowest), mnew = fmaxf(m[r], mx);
+      alpha[r] = __builtin_amdgcn_exp2f(m[r] - mnew);
+      m[r] = mnew;
+      const float p = see[r] ? __builtin_amdgcn_exp2f(s[r] - mnew) : 0.0f;
+      l[r] = fmaf(l[r], alpha[r], p);
+      const float top = fmaxf(__builtin_amdgcn_exp2f(mx - mnew) * vs_top, 0x1p-100f);
+      unit[r] = top * (1.0f / kDigits) * (PACKED ? 0.0625f : 1.0f);
+      // 2^23 + an integer of 23 bits: rounded to nearest by the sum; the digits' bytes are balanced as in digits4
+      const float x = fmaf(p, vs * (kDigits * __builtin_amdgcn_rcpf(top)), 8388608.0f);
+      const uint32_t u = (__float_as_uint(x) + 0x00808080u) ^ 0x00808080u;
+      put[(2 * R + r) * 64] = static_cast<uint8_t>(u);
+      put[(R + r) * 64] = static_cast<uint8_t>(u >> 8);
+      put[r * 64] = static_cast<uint8_t>(u >> 16);
+    }
+    wave_lds_order();
+    v4i p[3];
+#pragma unroll
+    for (int d = 0; d < 3; ++d) p[d] = *reinterpret_cast<const v4i *>(take + d * R * 64);
+    wave_lds_order();   // read before the next tile's are written
+#pragma unroll
+    for (int k = 0; k < HALVES; ++k) {
+      v4i e[4][3];
+      auto product = [&](v4i (&to)[3], v4i w) {
+#pragma unroll
+        for (int d = 0; d < 3; ++d) to[d] = mfma_i8(p[d], w, v4i{0, 0, 0, 0});
+      };
+#pragma unroll
+      for (int d = 0; d < BLOCKS; d += PACKED ? 2 : 1) {
+        const v4i x = values[PACKED ? (4 * k + d) / 2 : 4 * k + d];
+        if (PACKED) {
+          v4i lo4, hi4;
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            lo4[w] = static_cast<int>(static_cast<uint32_t>(x[w]) << 4 & 0xF0F0F0F0u);
+            hi4[w] = static_cast<int>(static_cast<uint32_t>(x[w]) & 0xF0F0F0F0u);
+          }
+          product(e[d], lo4);
+          product(e[d + 1], hi4);
+        } else {
+          product(e[d], x);
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        int d[3];
+#pragma unroll
+        for (int w = 0; w < 3; ++w)
+          d[w] = BLOCKS == 4 ? of_group(e[0][w][r], e[1][w][r], e[2 % BLOCKS][w][r], e[3 % BLOCKS][w][r], odd, upper) : odd ? e[1][w][r] : e[0][w][r];
+        o[k][r] = fmaf(joined(d[0], d[1], d[2]), unit[r], o[k][r] * alpha[r]);
+      }
+    }
+    load_values(next);
+  }
+
+  // the wavefronts' parts of the rows
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) l[r] += __shfl_xor(l[r], off, 64);
+    if (lane == 0) {
+      sm[wave][r] = m[r];
+      sl[wave][r] = l[r];
+    }
+#pragma unroll
+    for (int k = 0; k < HALVES; ++k)
+      if (lane < COLS) so[wave][r][64 * k + lane] = o[k][r];
+  }
+  __syncthreads();
+  uint32_t amax = 0u;
+  float *const left = part ? part + static_cast<int64_t>(blockIdx.x) * P::kFloats : nullptr;
+  for (int x = tid; x < R * COLS; x += kThreads) {
+    const int r = x / COLS, c = x % COLS, t = r / a.group;
+    float top = kLowest, sum = 0.0f, v = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, sm[w][r]);
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float weight = __builtin_amdgcn_exp2f(sm[w][r] - top);
+      sum = fmaf(sl[w][r], weight, sum);
+      v = fmaf(so[w][r][c], weight, v);
+    }
+    if (left) {
+      left[x] = v;
+      if (c == 0) {
+        left[P::kMax + r] = top;
+        left[P::kSum + r] = sum;
+      }
+    } else if (t < n && r < rows && c < g.dh) {
+      v *= sum == 0.0f ? 0.0f : 1.0f / sum;   // nothing seen: zeros
+      ctx[((b * a.T + t) * a.heads + h * a.group + r % a.group) * g.dh + c] = v;
+      amax = max(amax, __float_as_uint(v) & 0x7FFFFFFFu);
+    }
+  }
+  if (!left && absmax) put_absmax(absmax, amax);
+}
+
+template <int DT, bool PACKED>
+aqt_status launch_rows(const float *qkv, const CacheGeom &g, const CachedGeom &a, const int32_t *count, float *ctx, uint32_t *absmax,
+                       float *part, hipStream_t st) {
+  const int64_t rows = a.T * a.group;
+  const unsigned blocks = static_cast<unsigned>(g.streams * g.kv_heads * a.splits);
+  auto kern = rows == 1   ? attention_cached_few_kernel<DT, PACKED, 1>
+              : rows == 2 ? attention_cached_few_kernel<DT, PACKED, 2>
+                          : attention_cached_few_kernel<DT, PACKED, 4>;
+  kern<<<blocks, kThreads, 0, st>>>(qkv, g, a, count, ctx, absmax, part);
+  AQT_HIP(hipGetLastError());
+  return AQT_OK;
+}
+
+}  // namespace
+
+aqt_status launch_attention_cached_few(const float *qkv, const CacheGeom &g, const CachedGeom &a, const int32_t *count, float *ctx,
+                                       uint32_t *absmax, float *part, hipStream_t st) {
+  auto launch = g.packed ? (g.dh <= 32 ? launch_rows<2, true> : g.dh <= 64 ? launch_rows<4, true> : launch_rows<8, true>)
+                         : (g.dh <= 32 ? launch_rows<2, false> : g.dh <= 64 ? launch_rows<4, false> : launch_rows<8, false>);
+  return launch(qkv, g, a, count, ctx, absmax, part, st);
+}
+
+}  // namespace aqt

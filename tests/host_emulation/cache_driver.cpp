@@ -1,5 +1,5 @@
 // Driver of the host emulation of the kernels around positions and the quantized cache: the test splices cache.h, the kernels of
-// cache.hip (namespace cache_), attention_cached.hip (attend) and rotate.hip (turn) in front of this file.  Buffers are heap blocks of exactly the
+// cache.hip (namespace cache_), attention_cached.hip (attend), attention_cached_few.hip (few) and rotate.hip (turn) in front of this file.  Buffers are heap blocks of exactly the
 // sizes the kernels may touch, the cache starts out as NaNs in every reading, and results are compared with plain float64 loops.
 namespace aqt {
 static int bad = 0;
@@ -27,6 +27,24 @@ template <int L, bool VEC> static void read_(unsigned grid, const CacheGeom &g, 
   run(grid, 256, 0, [&] { cache_::cache_read_kernel<L, VEC>(g, pend, count, first, n, run_, per, k, v); });
 }
 
+template <int DT, bool PACKED> static void attention_as(const CacheGeom &g, int rows, const float *qkv, const CachedGeom &a, const int32_t *count, float *ctx, uint32_t *am, float *part) {
+  if (rows == 16) attend::attention_cached_kernel<DT, PACKED>(qkv, g, a, count, ctx, am, part);
+  else if (rows == 1) few::attention_cached_few_kernel<DT, PACKED, 1>(qkv, g, a, count, ctx, am, part);
+  else if (rows == 2) few::attention_cached_few_kernel<DT, PACKED, 2>(qkv, g, a, count, ctx, am, part);
+  else few::attention_cached_few_kernel<DT, PACKED, 4>(qkv, g, a, count, ctx, am, part);
+}
+static void attention(const CacheGeom &g, int rows, int cols, const float *qkv, const CachedGeom &a, const int32_t *count, float *ctx, uint32_t *am, float *part) {
+  if (g.packed) (cols == 32 ? attention_as<2, true> : cols == 64 ? attention_as<4, true> : attention_as<8, true>)(g, rows, qkv, a, count, ctx, am, part);
+  else (cols == 32 ? attention_as<2, false> : cols == 64 ? attention_as<4, false> : attention_as<8, false>)(g, rows, qkv, a, count, ctx, am, part);
+}
+template <int ROWS> static void join_as(int cols, const float *part, const CacheGeom &g, const CachedGeom &a, const int32_t *count, float *ctx, uint32_t *am) {
+  if (cols == 32) attend::attention_cached_join_kernel<ROWS, 32>(part, g, a, count, ctx, am);
+  else if (cols == 64) attend::attention_cached_join_kernel<ROWS, 64>(part, g, a, count, ctx, am);
+  else attend::attention_cached_join_kernel<ROWS, 128>(part, g, a, count, ctx, am);
+}
+static void join(int rows, int cols, const float *part, const CacheGeom &g, const CachedGeom &a, const int32_t *count, float *ctx, uint32_t *am) {
+  (rows == 1 ? join_as<1> : rows == 2 ? join_as<2> : rows == 4 ? join_as<4> : join_as<16>)(cols, part, g, a, count, ctx, am);
+}
 static void one(int streams, int64_t capacity, int heads, int kv, int dh, int bits, std::vector<int> steps, std::vector<std::pair<int, int>> windows, bool ragged) {
   printf("case %d streams, capacity %ld, heads %d / %d, dh %d, bits %d\n", streams, (long)capacity, heads, kv, dh, bits); fflush(stdout);
   const int cols = (heads + 2 * kv) * dh, qmax = (1 << (bits - 1)) - 1, group = heads / kv;
@@ -92,28 +110,24 @@ static void one(int streams, int64_t capacity, int heads, int kv, int dh, int bi
     free(first); free(rk); free(rv);
     // attention of the new frames
     for (auto [left, right] : windows) {
-      attend::CachedGeom a{};
-      a.T = T; a.ld = cols; a.heads = heads; a.group = group; a.row_tiles = (T * group + 15) / 16;
+      CachedGeom a{};
+      a.T = T; a.ld = cols; a.heads = heads; a.group = group;
       a.left = left; a.right = right; a.scale_log2e = (float)(1.4426950408889634 / sqrt((double)dh));
-      for (int splits : {1, 3}) {
-        a.splits = splits;
-        const int groups = streams * kv * a.row_tiles, COLS = attend::cols_of(dh);
+      // in tiles of 16 rows, and where they are few, each in its own place; by itself, and joined from three parts
+      for (int form = 0; form < 4; ++form) {
+        const int few_rows = T * group <= kFewRows ? (T * group == 1 ? 1 : T * group == 2 ? 2 : 4) : 0, rows = form & 2 ? few_rows : 16;
+        if (rows == 0) continue;
+        a.splits = form & 1 ? 3 : 1;
+        a.row_tiles = (T * group + rows - 1) / rows;
+        const int groups = streams * kv * a.row_tiles, COLS = attend::cols_of(dh), splits = a.splits;
         float *ctx = (float *)malloc((size_t)streams * T * heads * dh * 4);
-        const size_t pf = (size_t)groups * splits * (32 + 16 * COLS);
-        float *part = splits > 1 ? (float *)aligned_alloc(64, (pf * 4 + 63) / 64 * 64) : nullptr;
+        const size_t pf = (size_t)groups * splits * ((rows * COLS + 2 * rows + 3) / 4 * 4);
+        float *part = splits > 1 ? (float *)aligned_alloc(16, (pf * 4 + 15) / 16 * 16) : nullptr;
         for (size_t i = 0; i < (size_t)streams * T * heads * dh; ++i) ctx[i] = 77.0f;
         uint32_t am = 0;
         const unsigned grid = (unsigned)(groups * splits);
-        auto kern = [&] {
-          if (g.packed) { if (COLS == 32) attend::attention_cached_kernel<2, true>(qkv, g, a, count, ctx, &am, part); else if (COLS == 64) attend::attention_cached_kernel<4, true>(qkv, g, a, count, ctx, &am, part); else attend::attention_cached_kernel<8, true>(qkv, g, a, count, ctx, &am, part); }
-          else { if (COLS == 32) attend::attention_cached_kernel<2, false>(qkv, g, a, count, ctx, &am, part); else if (COLS == 64) attend::attention_cached_kernel<4, false>(qkv, g, a, count, ctx, &am, part); else attend::attention_cached_kernel<8, false>(qkv, g, a, count, ctx, &am, part); }
-        };
-        run(grid, 256, 0, kern);
-        if (part) run((unsigned)groups, 256, 0, [&] {
-          if (COLS == 32) attend::attention_cached_join_kernel<32>(part, g, a, count, ctx, &am);
-          else if (COLS == 64) attend::attention_cached_join_kernel<64>(part, g, a, count, ctx, &am);
-          else attend::attention_cached_join_kernel<128>(part, g, a, count, ctx, &am);
-        });
+        run(grid, 256, 0, [&] { attention(g, rows, COLS, qkv, a, count, ctx, &am, part); });
+        if (part) run((unsigned)groups, 256, 0, [&] { join(rows, COLS, part, g, a, count, ctx, &am); });
         double worst = 0, largest = 0;
         for (int b = 0; b < streams; ++b) for (int t = 0; t < T; ++t) for (int h = 0; h < heads; ++h) {
           const float *got = ctx + ((size_t)(b * T + t) * heads + h) * dh;
@@ -140,7 +154,7 @@ static void one(int streams, int64_t capacity, int heads, int kv, int dh, int bi
           }
           for (int e = 0; e < dh; ++e) { at_least(worst, fabs(got[e] - ref_o[e]) / mag); at_least(largest, (double)fabsf(got[e])); }
         }
-        printf("  T %d window %d %d splits %d: worst error / sum of magnitudes %.3g\n", T, left, right, splits, worst);
+        printf("  T %d window %d %d splits %d rows %d: worst error / sum of magnitudes %.3g\n", T, left, right, splits, rows, worst);
         if (!(worst < 4e-6)) complain("attention");
         if (__float_as_uint((float)largest) != am) complain("absmax");
         free(ctx); free(part);
@@ -244,9 +258,9 @@ int main(int argc, char **) {
     one(3, 64, 1, 1, 64, 8, {5, 62, 1, 70}, {{-1, 0}, {7, 3}}, true);
     one(1, 128, 4, 2, 36, 4, {17, 120, 4}, {{-1, -1}, {0, 0}}, false);
     one(1, 64, 6, 1, 128, 4, {3, 1}, {{2, 0}, {-1, 2}}, false);
-    one(2, 64, 1, 1, 5, 6, {4, 66}, {{-1, 0}}, true);
+    one(2, 64, 1, 1, 5, 6, {4, 66, 3}, {{-1, 0}}, true);
     one(1, 128, 1, 1, 80, 3, {60, 100}, {{30, 1}}, false);
-    one(1, 64, 2, 1, 128, 8, {9}, {{-1, 0}}, false);
+    one(1, 64, 2, 1, 128, 8, {9, 1}, {{-1, 0}}, false);
     one(2, 64, 40, 2, 16, 2, {3, 1}, {{-1, 0}, {1, 1}}, true);
   }
   printf(bad ? "MISMATCH\n" : "ok\n");

@@ -6,7 +6,7 @@ import subprocess
 
 import pytest
 
-from test_kernels_on_host import HERE, ROOT, read, rule
+from test_kernels_on_host import HERE, ROOT, cut, read, rule
 
 
 def spliced():
@@ -16,13 +16,25 @@ def spliced():
 
     layout = read("cache.h")
     layout = layout[:layout.index("bool cache_shape_ok")] + rule("cache.hip", "CacheGeom cache_geom(") + "}\n"
+    shared = cut(read("attention_cached.h"), "// part: the splits' rows", "namespace {")
     helpers = "namespace aqt {\n" + "".join(rule_line + "\n" for rule_line in (
         "inline int qmax_of(int bits) { return (1 << (bits - 1)) - 1; }", "inline bool packed4(int bits_w) { return bits_w <= 4; }")) + "}\n"
     shim = ('#define AQT_ON_HOST 1\n#include "vectors_on_host.h"\n#include "aqt.h"\n'
+            "inline int __builtin_amdgcn_readlane(int v, int lane) { return lane_value(v, (unsigned)lane); }\n"
+            # the data-parallel primitives of a maximum over the wavefront: row_shr:n, row_bcast:15, row_bcast:31
+            "inline int __builtin_amdgcn_update_dpp(int old, int v, int ctrl, int, int, bool) {\n"
+            "  const unsigned l = threadIdx.x & 63u;\n"
+            "  const bool shift = ctrl < 0x120, on = shift ? (l & 15u) >= (unsigned)(ctrl & 15) : ctrl == 0x142 ? l >= 16u : l >= 32u;\n"
+            "  const int from = lane_value(v, on ? (shift ? l - (unsigned)(ctrl & 15) : ctrl == 0x142 ? (l & 48u) - 1u : 31u) : l);\n"
+            "  return on ? from : old;\n}\n"
             "inline float __builtin_amdgcn_rsqf(float x) { return 1.0f / sqrtf(x); }\n"
             "inline float __shfl(float v, int lane) { return lane_value(v, (unsigned)lane); }\n")
+    # a vector of two or four ints, by its length
+    shim += "template <int N> struct key_piece_of { typedef v4i type; };\ntemplate <> struct key_piece_of<2> { typedef v2i type; };\n"
     return (shim + helpers + layout + read("quant_code.h") + kernels("cache.hip", "cache_", "}  // namespace\n\nbool cache_shape_ok") +
-            kernels("attention_cached.hip", "attend", "// Workgroups that share the tiles of 16 rows.") +
+            shared + kernels("attention_cached_few.hip", "few", "template <int DT, bool PACKED>\naqt_status launch_rows").replace(
+                "typedef int key_piece __attribute__((ext_vector_type(KEYS)));", "typedef typename key_piece_of<KEYS>::type key_piece;") +
+            kernels("attention_cached.hip", "attend", "// How a call is cut up: rows of a workgroup") +
             kernels("rotate.hip", "turn", "__global__ void rotation_turns_kernel") +
             open(os.path.join(HERE, "host_emulation", "cache_driver.cpp")).read())
 
