@@ -12,7 +12,7 @@ struct CachedGeom {
   float scale_log2e;
 };
 // Wavefronts per SIMD that the kernel's registers are shared out to, without spills (dt: blocks of 16 head columns, r: rows).
-constexpr int few_waves(int dt, bool packed, int r) { return dt == 8 ? (packed && r < 4 ? 3 : 2) : r == 4 && !packed ? 3 : 4; }
+constexpr int few_waves(int dt, bool packed, int r) { return dt == 8 ? (packed && r < 4 ? 3 : 2) : r > 1 && !packed ? 3 : 4; }
 constexpr int kFewRows = 4;   // rows per key / value head and stream up to which attention_cached_few.hip takes the call
 // part: the splits' rows, [rows][columns], then maxima and sums [rows] each, one after the other (nullptr: straight to ctx)
 aqt_status launch_attention_cached_few(const float *qkv, const CacheGeom &g, const CachedGeom &a, const int32_t *count, float *ctx,
@@ -39,6 +39,20 @@ __device__ __forceinline__ void digits4(const int (&n)[4], int &d0, int &d1, int
   d0 = static_cast<int>(__builtin_amdgcn_perm(ct, at, 0x05040100u));
 }
 
+// A weight of 0 .. 1 as an integer w of 23 bits: 0x808080 + w, as a float of the binade 2^23 .. 2^24, whose steps are ones; the
+// sum rounds to nearest.  Its bytes are the balanced digits (the highest lacks the sign bit that the exponent's place took; the others
+// are off by 128, i.e. by their highest bit).
+__device__ __forceinline__ uint32_t weight_bits(float weight, float to) { return __float_as_uint(fmaf(weight, to, 8421504.0f)); }
+
+// Four of them, a dword of each digit.
+__device__ __forceinline__ void weight_digits4(const uint32_t (&u)[4], int &d0, int &d1, int &d2) {
+  const uint32_t ab = __builtin_amdgcn_perm(u[1], u[0], 0x05010400u), cd = __builtin_amdgcn_perm(u[3], u[2], 0x05010400u);   // a0 b0 a1 b1
+  const uint32_t at = __builtin_amdgcn_perm(u[1], u[0], 0x0C0C0602u), ct = __builtin_amdgcn_perm(u[3], u[2], 0x0C0C0602u);   // a2 b2
+  d2 = static_cast<int>(__builtin_amdgcn_perm(cd, ab, 0x05040100u) ^ 0x80808080u);
+  d1 = static_cast<int>(__builtin_amdgcn_perm(cd, ab, 0x07060302u) ^ 0x80808080u);
+  d0 = static_cast<int>(__builtin_amdgcn_perm(ct, at, 0x05040100u));
+}
+
 __device__ __forceinline__ v4i mfma_i8(v4i a, v4i b, v4i c) { return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0); }
 
 // The three digits' sums as one number, 256^2 a + 256 b + c.
@@ -49,6 +63,25 @@ __device__ __forceinline__ float joined(int a, int b, int c) {
 __device__ __forceinline__ float max_of_groups(float v) {   // over the four lanes of a row
   v = fmaxf(v, __shfl_xor(v, 16, 64));
   return fmaxf(v, __shfl_xor(v, 32, 64));
+}
+
+// The largest of a wavefront's 64 words.  (The steps fuse with the moves between lanes, as they do not for float32.)
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+  auto step = [&](int w) { v = max(v, static_cast<uint32_t>(w)); };
+  step(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), 0x111, 0xF, 0xF, true));   // row_shr:1, 2, 4, 8: a row's last lane has its largest
+  step(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), 0x112, 0xF, 0xF, true));
+  step(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), 0x114, 0xF, 0xF, true));
+  step(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), 0x118, 0xF, 0xF, true));
+  step(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), 0x142, 0xA, 0xF, false));  // row_bcast:15 into rows 1 and 3, row_bcast:31 into 2 and 3
+  step(__builtin_amdgcn_update_dpp(0, static_cast<int>(v), 0x143, 0xC, 0xF, false));
+  return static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(v), 63));
+}
+// Of floats: as they are where none is negative, otherwise as words in their order.
+__device__ __forceinline__ float wave_max_positive(float v) { return __uint_as_float(wave_max(__float_as_uint(v))); }
+__device__ __forceinline__ float wave_max_signed(float v) {
+  const uint32_t u = __float_as_uint(v);
+  const uint32_t w = wave_max(u ^ (static_cast<uint32_t>(static_cast<int>(u) >> 31) | 0x80000000u));
+  return __uint_as_float(w ^ (w >> 31 ? 0x80000000u : 0xFFFFFFFFu));
 }
 
 // Four columns of a row of ctx.

@@ -21,55 +21,119 @@ namespace aqt {
 namespace {
 
 constexpr int kRows = 16;                 // rows of a workgroup
-constexpr int64_t kWorkgroups = 2048;
+// Wavefronts per SIMD that the kernel's registers are shared out to, without spills (dt: blocks of 16 head columns).
+constexpr int many_waves(int dt, bool packed) { return dt == 8 ? 2 : dt == 2 || packed ? 4 : 3; }
+
+// The workgroup's place: (stream and head, row tile, split).  The row tiles of a split read the same codes; workgroup ids eight apart run
+// on one XCD, so that with a multiple of eight of them the row tiles of a split are given to one XCD's L2.
+struct Place {
+  int bh, rt, split;
+};
+__device__ __forceinline__ Place place_of(const CachedGeom &a, int64_t heads) {
+  const int id = static_cast<int>(blockIdx.x);
+  const int64_t lanes = heads * a.splits;   // of row tiles
+  int lane, rt;
+  if (lanes % 8 == 0) {
+    lane = id / (8 * a.row_tiles) * 8 + id % 8;
+    rt = id / 8 % a.row_tiles;
+  } else {
+    lane = id / a.row_tiles;
+    rt = id % a.row_tiles;
+  }
+  return Place{lane / a.splits, rt, lane % a.splits};
+}
 
 // DT: blocks of 16 head columns that a workgroup holds (2, 4 or 8)
 template <int DT, bool PACKED>
-__global__ __launch_bounds__(kThreads, 2) void attention_cached_kernel(const float *__restrict__ qkv, CacheGeom g, CachedGeom a,
+__global__ __launch_bounds__(kThreads, many_waves(DT, PACKED)) void attention_cached_kernel(const float *__restrict__ qkv, CacheGeom g, CachedGeom a,
                                                                        const int32_t *__restrict__ count, float *__restrict__ ctx,
                                                                        uint32_t *__restrict__ absmax, float *__restrict__ part) {
   constexpr int KS = DT == 8 ? 2 : 1;        // steps of 64 head columns
   constexpr int COLS = 16 * DT, LD = COLS + 4;
+  constexpr int KEYS = PACKED ? 2 : 4, VALUES = PACKED ? DT / 2 : DT;
+  using P = Partial<kRows, COLS>;
   __shared__ __attribute__((aligned(16))) float so[kWaves][kRows][LD];
+  __shared__ __attribute__((aligned(16))) float scales[kWaves][128];
   __shared__ float sm[kWaves][kRows], sl[kWaves][kRows];
   const int tid = static_cast<int>(threadIdx.x), lane = tid & 63, lr = lane & 15, lg = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  int64_t id = blockIdx.x;
-  const int split = static_cast<int>(id % a.splits);
-  id /= a.splits;
-  const int rt = static_cast<int>(id % a.row_tiles);
-  id /= a.row_tiles;
-  const int h = static_cast<int>(id % g.kv_heads);
-  const int64_t b = id / g.kv_heads;
+  const Place pl = place_of(a, g.streams * g.kv_heads);
+  const int h = pl.bh % g.kv_heads;
+  const int64_t b = pl.bh / g.kv_heads;
   const StreamFrames f = stream_frames(g, count, a.T, b);
   const int n = static_cast<int>(f.end - f.length);
-  const int t_first = rt * kRows / a.group;
+  const int row0 = pl.rt * kRows, t_first = row0 / a.group;
   if (t_first >= n) return;                  // frames that the stream did not bring: their rows stay as they are
-  const int t_last = min((rt * kRows + kRows - 1) / a.group, n - 1);
+  const int t_last = min((row0 + kRows - 1) / a.group, n - 1);
 
-  // the frames that the workgroup's rows see, and this lane's row; counted from the first tile
+  // the frames that the workgroup's rows see, and this lane's rows; counted from the first tile
   auto from = [&](int t) { const int64_t x = f.length + t - a.left; return a.left < 0 || x < f.oldest ? f.oldest : x; };
   auto upto = [&](int t) { const int64_t x = f.length + t + a.right; return a.right < 0 || x > f.end - 1 ? f.end - 1 : x; };
   const int64_t first = from(t_first), last = upto(t_last), tile0 = first >> 6, base = tile0 * 64;
   const int tiles = last < first ? 0 : static_cast<int>((last >> 6) - tile0) + 1;
-  const int row = rt * kRows + lr, t_own = min(row / a.group, n - 1);   // rows behind the last repeat it and are not stored
-  const int lo = static_cast<int>(from(t_own) - base), hi = static_cast<int>(upto(t_own) - base);
+  const int first_seen = static_cast<int>(first - base), last_seen = static_cast<int>(last - base);
   const int all_lo = static_cast<int>(from(t_last) - base), all_hi = static_cast<int>(upto(t_first) - base);
 
-  // the row's digits: 16 columns per lane and step
+  // the rows: 16 columns per lane and step, requested in front of the first tile, so that their digits are formed under its trip from memory
+  const int row = row0 + lr, t_own = min(row / a.group, n - 1);   // rows behind the last repeat it and are not stored
+  const int lo = static_cast<int>(from(t_own) - base), hi = static_cast<int>(upto(t_own) - base);
+  float x[KS][16];
+  {
+    const float *const src = qkv + (b * a.T + t_own) * a.ld + (static_cast<int64_t>(h) * a.group + row % a.group) * g.dh;
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x[k][i] = src[min(64 * k + 16 * lg + i, g.dh - 1)];
+  }
+
+  // A tile's codes and scales are requested where the tile before has given up their registers: the keys' trip from memory passes
+  // under the rest of that tile, the values' under this one's scores (8 streams of 128 rows: 66 us with both at the head of a tile, 63 so).
+  typedef int key_piece __attribute__((ext_vector_type(KEYS)));
+  key_piece keys[4][KS];
+  v4i values[VALUES];
+  float ks_next, vs_next;
+  auto load_keys = [&](const uint8_t *tile) {
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {   // sixteen columns to a lane; one beyond the row meets digits of zero
+        const int at = (64 * k + 16 * lg) * KEYS / 4;
+        keys[t][k] = *reinterpret_cast<const key_piece *>(tile + (16 * t + lr) * g.key_row + (at < g.key_row ? at : 0));
+      }
+    ks_next = reinterpret_cast<const float *>(tile + cache_scales(g))[lane];
+    vs_next = reinterpret_cast<const float *>(tile + cache_scales(g))[64 + lane];
+  };
+  auto load_values = [&](const uint8_t *tile) {
+#pragma unroll
+    for (int d = 0; d < VALUES; ++d) {
+      const int at = 16 * d + lr;      // columns beyond the head are not stored
+      values[d] = *reinterpret_cast<const v4i *>(tile + cache_values(g) + (at < g.value_rows ? at : lr) * 64 + 16 * lg);
+    }
+  };
+
+  const uint8_t *const head = g.data + (b * g.kv_heads + h) * g.tiles * static_cast<int64_t>(g.tile_bytes);
+  const int step = a.splits * kWaves, slot_step = step % g.tiles;
+  float m = kLowest, l = 0.0f;
+  v4f o[DT];                                 // element r of block d: column 16 d + 4 lg + r of this lane's row
+#pragma unroll
+  for (int d = 0; d < DT; ++d) o[d] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+  int i = pl.split * kWaves + wave;
+  int slot = tile_slot(tile0 + i, g.tiles);
+  if (i < tiles) {
+    const uint8_t *const tile = head + static_cast<int64_t>(slot) * g.tile_bytes;
+    load_keys(tile);
+    load_values(tile);
+  }
+  // their digits
   v4i q[KS][3];
   float row_scale;
   {
-    const float *const src = qkv + (b * a.T + t_own) * a.ld + (static_cast<int64_t>(h) * a.group + row % a.group) * g.dh;
-    float x[KS][16];
     uint32_t m = 0u;
 #pragma unroll
     for (int k = 0; k < KS; ++k)
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        const int c = 64 * k + 16 * lg + i;
-        x[k][i] = src[min(c, g.dh - 1)];
-        x[k][i] = c < g.dh ? x[k][i] : 0.0f;
+        x[k][i] = 64 * k + 16 * lg + i < g.dh ? x[k][i] : 0.0f;
         m = max(m, __float_as_uint(x[k][i]) & 0x7FFFFFFFu);
       }
     m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 16, 64)));
@@ -92,121 +156,114 @@ __global__ __launch_bounds__(kThreads, 2) void attention_cached_kernel(const flo
       }
   }
 
-  const uint8_t *const head = g.data + (b * g.kv_heads + h) * g.tiles * static_cast<int64_t>(g.tile_bytes);
-  const int step = a.splits * kWaves, slot_step = step % g.tiles;
-  float m = kLowest, l = 0.0f;
-  v4f o[DT];                                 // element r of block d: column 16 d + 4 lg + r of this lane's row
-#pragma unroll
-  for (int d = 0; d < DT; ++d) o[d] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-  int i = split * kWaves + wave;
-  int slot = tile_slot(tile0 + i, g.tiles);
   for (; i < tiles; i += step) {
-    const uint8_t *const tile = head + static_cast<int64_t>(slot) * g.tile_bytes;
-    slot += slot_step;
-    slot = slot >= g.tiles ? slot - g.tiles : slot;
-    const float *const scales = reinterpret_cast<const float *>(tile + cache_scales(g));
-    // scores
-    float s[16];
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      v4i c[3];
-#pragma unroll
-      for (int d = 0; d < 3; ++d) c[d] = v4i{0, 0, 0, 0};
-      const uint8_t *const key = tile + (16 * t + lr) * g.key_row;
-#pragma unroll
-      for (int k = 0; k < KS; ++k) {
-        v4i w;
-        if (PACKED) {   // sixteen columns in eight bytes; a lane beyond the row meets digits of zero
-          const int at = 32 * k + 8 * lg;
-          const v2i x = *reinterpret_cast<const v2i *>(key + (at < g.key_row ? at : 0));
-          w = v4i{static_cast<int>(static_cast<uint32_t>(x.x) << 4 & 0xF0F0F0F0u), static_cast<int>(static_cast<uint32_t>(x.y) << 4 & 0xF0F0F0F0u),
-                  static_cast<int>(static_cast<uint32_t>(x.x) & 0xF0F0F0F0u), static_cast<int>(static_cast<uint32_t>(x.y) & 0xF0F0F0F0u)};
-        } else {
-          const int at = 64 * k + 16 * lg;
-          w = *reinterpret_cast<const v4i *>(key + (at < g.key_row ? at : 0));
-        }
-#pragma unroll
-        for (int d = 0; d < 3; ++d) c[d] = mfma_i8(w, q[k][d], c[d]);
-      }
-      const v4f ks = *reinterpret_cast<const v4f *>(scales + 16 * t + 4 * lg);
-      const float kse[4] = {ks.x, ks.y, ks.z, ks.w};
-#pragma unroll
-      for (int r = 0; r < 4; ++r) s[4 * t + r] = joined(c[0][r], c[1][r], c[2][r]) * (row_scale * kse[r]);
+    if (i + step < tiles) {   // otherwise this tile's once more: never another's memory
+      slot += slot_step;
+      slot = slot >= g.tiles ? slot - g.tiles : slot;
     }
-    // window: what it hides, and what is no frame of the stream's, may hold anything
+    const uint8_t *const next = head + static_cast<int64_t>(slot) * g.tile_bytes;
     const int j0 = 64 * i;
-    uint32_t seen = 0xFFFFu;
-    if (j0 < all_lo || j0 + 63 > all_hi) {
-      seen = 0u;
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int j = j0 + 16 * (e >> 2) + 4 * lg + (e & 3);
-        seen |= (j >= lo && j <= hi ? 1u : 0u) << e;
-      }
-    }
-    float mx = kLowest;
-#pragma unroll
-    for (int e = 0; e < 16; ++e) mx = fmaxf(mx, seen >> e & 1u ? s[e] : kLowest);
-    mx = max_of_groups(mx);
-    const float mnew = fmaxf(m, mx), alpha = __builtin_amdgcn_exp2f(m - mnew);
-    m = mnew;
-    l *= alpha;
-    // probabilities, times the values' scales, and their digits
-    float top = 0.0f;
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      const v4f vs = *reinterpret_cast<const v4f *>(scales + 64 + 16 * t + 4 * lg);
-      const float vse[4] = {vs.x, vs.y, vs.z, vs.w};
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int e = 4 * t + r;
-        const bool see = seen >> e & 1u;
-        const float p = see ? __builtin_amdgcn_exp2f(s[e] - m) : 0.0f;
-        l += p;
-        s[e] = see ? p * vse[r] : 0.0f;
-        top = fmaxf(top, s[e]);
-      }
-    }
-    top = fmaxf(max_of_groups(top), 0x1p-100f);
-    const float to = kDigits / top;
+    const bool whole = j0 >= all_lo && j0 + 63 <= all_hi;
+    // the frames' scales go round through LDS: a lane's frames are 16 t + 4 lg + r
+    float *const sc = scales[wave];
+    const float vs = j0 + lane >= first_seen && j0 + lane <= last_seen ? vs_next : 0.0f;   // others may hold anything
+    sc[lane] = ks_next;
+    sc[64 + lane] = vs;
+    const float vs_top = wave_max_positive(vs);
+    wave_lds_order();
     v4i p[3];
+    float unit;
+    {
+      // scores
+      float s[16];
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      int nn[4];
+      for (int t = 0; t < 4; ++t) {
+        v4i c[3];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) nn[r] = static_cast<int>(rintf(s[4 * t + r] * to));
-      int d0, d1, d2;
-      digits4(nn, d0, d1, d2);
-      p[0][t] = d0;
-      p[1][t] = d1;
-      p[2][t] = d2;
+        for (int k = 0; k < KS; ++k) {
+          v4i w;
+          if constexpr (PACKED) {
+            const uint32_t x = static_cast<uint32_t>(keys[t][k][0]), y = static_cast<uint32_t>(keys[t][k][1]);
+            w = v4i{static_cast<int>(x << 4 & 0xF0F0F0F0u), static_cast<int>(y << 4 & 0xF0F0F0F0u), static_cast<int>(x & 0xF0F0F0F0u),
+                    static_cast<int>(y & 0xF0F0F0F0u)};
+          } else {
+            w = keys[t][k];
+          }
+#pragma unroll
+          for (int d = 0; d < 3; ++d) c[d] = mfma_i8(w, q[k][d], k == 0 ? v4i{0, 0, 0, 0} : c[d]);
+        }
+        const v4f ks = *reinterpret_cast<const v4f *>(&sc[16 * t + 4 * lg]);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) s[4 * t + r] = joined(c[0][r], c[1][r], c[2][r]) * ks[r] * row_scale;
+      }
+      load_keys(next);
+      if (!whole) {   // what the window hides, and what is no frame of the stream's, may hold anything
+        asm volatile("");   // a branch: as selections they would be taken in every tile
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int j = j0 + 16 * (e >> 2) + 4 * lg + (e & 3);
+          s[e] = j >= lo && j <= hi ? s[e] : -__builtin_inff();
+        }
+      }
+      float mx = kLowest;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[e]);
+      mx = max_of_groups(mx);
+      if (__any(mx > m)) {
+        const float mnew = fmaxf(m, mx), alpha = __builtin_amdgcn_exp2f(m - mnew);
+        m = mnew;
+        l *= alpha;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) o[d][r] *= alpha;
+      }
+      // Probabilities, and their digits times the values' scales: relative to the largest probability times the largest scale, a
+      // bound of the largest weight.
+      const float top = fmaxf(__builtin_amdgcn_exp2f(mx - m) * vs_top, 0x1p-100f);
+      const float to = kDigits * __builtin_amdgcn_rcpf(top);
+      unit = top * (1.0f / kDigits) * (PACKED ? 0.0625f : 1.0f);
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const v4f vs4 = *reinterpret_cast<const v4f *>(&sc[64 + 16 * t + 4 * lg]);
+        uint32_t w[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float e = __builtin_amdgcn_exp2f(s[4 * t + r] - m);
+          l += e;
+          w[r] = weight_bits(e, vs4[r] * to);
+        }
+        int d0, d1, d2;
+        weight_digits4(w, d0, d1, d2);
+        p[0][t] = d0;
+        p[1][t] = d1;
+        p[2][t] = d2;
+      }
     }
-    const float unit = top * (1.0f / kDigits) * (PACKED ? 0.0625f : 1.0f);
-    const uint8_t *const values = tile + cache_values(g) + 16 * lg;
-    auto add = [&](v4f &to_o, v4i w) {
+    wave_lds_order();   // the scales are read before the next tile's are written
+    auto add = [&](int d, v4i w) {
       v4i c[3];
 #pragma unroll
-      for (int d = 0; d < 3; ++d) c[d] = mfma_i8(w, p[d], v4i{0, 0, 0, 0});
+      for (int e = 0; e < 3; ++e) c[e] = mfma_i8(w, p[e], v4i{0, 0, 0, 0});
 #pragma unroll
-      for (int r = 0; r < 4; ++r) to_o[r] = fmaf(joined(c[0][r], c[1][r], c[2][r]), unit, to_o[r] * alpha);
+      for (int r = 0; r < 4; ++r) o[d][r] = fmaf(joined(c[0][r], c[1][r], c[2][r]), unit, o[d][r]);
     };
 #pragma unroll
-    for (int d = 0; d < DT; d += PACKED ? 2 : 1) {
-      const int at = 16 * (PACKED ? d / 2 : d) + lr;
-      const v4i x = *reinterpret_cast<const v4i *>(values + (at < g.value_rows ? at : lr) * 64);   // columns beyond the head are not stored
-      if (PACKED) {
+    for (int d = 0; d < VALUES; ++d) {
+      if constexpr (PACKED) {
         v4i lo4, hi4;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          lo4[e] = static_cast<int>(static_cast<uint32_t>(x[e]) << 4 & 0xF0F0F0F0u);
-          hi4[e] = static_cast<int>(static_cast<uint32_t>(x[e]) & 0xF0F0F0F0u);
+          lo4[e] = static_cast<int>(static_cast<uint32_t>(values[d][e]) << 4 & 0xF0F0F0F0u);
+          hi4[e] = static_cast<int>(static_cast<uint32_t>(values[d][e]) & 0xF0F0F0F0u);
         }
-        add(o[d], lo4);
-        add(o[d + 1], hi4);
+        add(2 * d, lo4);
+        add(2 * d + 1, hi4);
       } else {
-        add(o[d], x);
+        add(d, values[d]);
       }
     }
+    load_values(next);
   }
 
   // the wavefronts' parts of the rows
@@ -219,6 +276,8 @@ __global__ __launch_bounds__(kThreads, 2) void attention_cached_kernel(const flo
 #pragma unroll
   for (int d = 0; d < DT; ++d) *reinterpret_cast<v4f *>(&so[wave][lr][16 * d + 4 * lg]) = o[d];
   __syncthreads();
+  uint32_t amax = 0u;
+  float *const left = part ? part + ((static_cast<int64_t>(pl.bh) * a.row_tiles + pl.rt) * a.splits + pl.split) * P::kFloats : nullptr;
   const int orow = tid >> 4;
   float top = kLowest, sum = 0.0f, weight[kWaves];
 #pragma unroll
@@ -228,12 +287,9 @@ __global__ __launch_bounds__(kThreads, 2) void attention_cached_kernel(const flo
     weight[w] = __builtin_amdgcn_exp2f(sm[w][orow] - top);
     sum = fmaf(sl[w][orow], weight[w], sum);
   }
-  const int out_row = rt * kRows + orow, t = out_row / a.group;
-  const bool store = t < n;
+  const int out_row = row0 + orow, t = out_row / a.group;
   float *const to = ctx + ((b * a.T + t) * a.heads + h * a.group + out_row % a.group) * g.dh;
-  float *const left = part ? part + static_cast<int64_t>(blockIdx.x) * Partial<kRows, COLS>::kFloats : nullptr;
   const float inv = sum == 0.0f ? 0.0f : 1.0f / sum;   // nothing seen: zeros
-  uint32_t amax = 0u;
 #pragma unroll
   for (int c = 4 * (tid & 15); c < COLS; c += 64) {
     v4f v = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -245,7 +301,7 @@ __global__ __launch_bounds__(kThreads, 2) void attention_cached_kernel(const flo
     }
     if (left) {
       *reinterpret_cast<v4f *>(left + orow * COLS + c) = v;
-    } else if (store) {
+    } else if (t < n) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[e] *= inv;
       amax = max(amax, put_ctx(to, c, g.dh, v));
@@ -253,8 +309,8 @@ __global__ __launch_bounds__(kThreads, 2) void attention_cached_kernel(const flo
   }
   if (left) {
     if ((tid & 15) == 0) {
-      left[Partial<kRows, COLS>::kMax + orow] = top;
-      left[Partial<kRows, COLS>::kSum + orow] = sum;
+      left[P::kMax + orow] = top;
+      left[P::kSum + orow] = sum;
     }
   } else if (absmax) {
     put_absmax(absmax, amax);
@@ -359,14 +415,14 @@ struct CachedCut {
 // window: the longest run of frames that a row tile sees
 CachedCut cut_of(const CacheGeom &g, int64_t rows, int64_t window) {
   CachedCut c;
+  const int dt = cols_of(g.dh) / 16;
   c.rows = rows <= kFewRows ? (rows == 1 ? 1 : rows == 2 ? 2 : 4) : kRows;
   c.row_tiles = static_cast<int>(cdiv(rows, c.rows));
   c.groups = g.streams * g.kv_heads * c.row_tiles;
-  // Few rows: as many workgroups as the chip holds at a time, a wavefront of each on every SIMD; what comes behind them would form
-  // its rows' digits and request its first tile while the others are at the memory's rate (32 streams, four rows of 128 columns:
-  // 108 us with 512 workgroups, 113 with 1024, 123 with 2048).  Sixteen rows are bound by vector instructions, and a workgroup's share
-  // had better be small (8 streams of 128 rows: 76 us with 2048, 80 with 1024, 83 with 512).
-  const int64_t want = c.rows == kRows ? cdiv(kWorkgroups, c.groups) : 256 * few_waves(cols_of(g.dh) / 16, g.packed, c.rows) / c.groups;
+  // As many workgroups as the chip holds at a time, a wavefront of each on every SIMD: what comes behind them would form its rows' digits
+  // and request its first tile while the others work (32 streams, four rows of 128 columns: 108 us with 512 workgroups, 113 with
+  // 1024, 123 with 2048; 8 streams of 128 rows: 64 us with 512, 67 with 1024, 74 with 2048).
+  const int64_t want = 256 * (c.rows <= kFewRows ? few_waves(dt, g.packed, c.rows) : many_waves(dt, g.packed)) / c.groups;
   const int64_t most = cdiv(cdiv(window, 64) + 1, kWaves), s = want < most ? want : most;
   c.splits = static_cast<int>(s < 1 ? 1 : s);
   return c;
@@ -420,7 +476,8 @@ aqt_status launch_attention_cached(const float *qkv, int64_t T, int heads, const
     AQT_HIP(hipGetLastError());
   }
   float *const part = cut.splits > 1 ? static_cast<float *>(ws) : nullptr;
-  if (cut.rows != kRows) {
+  const unsigned blocks = static_cast<unsigned>(cut.groups * cut.splits);
+  if (cut.rows <= kFewRows) {
     AQT_TRY(launch_attention_cached_few(qkv, g, a, count, ctx, absmax, part, st));
   } else {
     auto kern = g.packed ? (c.dh <= 32   ? attention_cached_kernel<2, true>
@@ -429,7 +486,7 @@ aqt_status launch_attention_cached(const float *qkv, int64_t T, int heads, const
                          : (c.dh <= 32   ? attention_cached_kernel<2, false>
                             : c.dh <= 64 ? attention_cached_kernel<4, false>
                                          : attention_cached_kernel<8, false>);
-    kern<<<static_cast<unsigned>(cut.groups * cut.splits), kThreads, 0, st>>>(qkv, g, a, count, ctx, absmax, part);
+    kern<<<blocks, kThreads, 0, st>>>(qkv, g, a, count, ctx, absmax, part);
     AQT_HIP(hipGetLastError());
   }
   if (!part) return AQT_OK;

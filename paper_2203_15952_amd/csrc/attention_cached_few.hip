@@ -14,18 +14,6 @@
 namespace aqt {
 namespace {
 
-// The largest of a wavefront's 64 values, in every lane.
-__device__ __forceinline__ float wave_max(float v) {
-  auto step = [&](int w) { v = fmaxf(v, __uint_as_float(static_cast<uint32_t>(w))); };
-  const auto bits = [&] { return static_cast<int>(__float_as_uint(v)); };
-  step(__builtin_amdgcn_update_dpp(bits(), bits(), 0x111, 0xF, 0xF, false));   // row_shr:1, 2, 4, 8: a row's last lane has its maximum
-  step(__builtin_amdgcn_update_dpp(bits(), bits(), 0x112, 0xF, 0xF, false));
-  step(__builtin_amdgcn_update_dpp(bits(), bits(), 0x114, 0xF, 0xF, false));
-  step(__builtin_amdgcn_update_dpp(bits(), bits(), 0x118, 0xF, 0xF, false));
-  step(__builtin_amdgcn_update_dpp(bits(), bits(), 0x142, 0xF, 0xF, false));   // row_bcast:15, 31
-  step(__builtin_amdgcn_update_dpp(bits(), bits(), 0x143, 0xF, 0xF, false));
-  return __uint_as_float(static_cast<uint32_t>(__builtin_amdgcn_readlane(bits(), 63)));
-}
 __device__ __forceinline__ float of_lane(float v, int lane) {
   return __uint_as_float(static_cast<uint32_t>(__builtin_amdgcn_readlane(static_cast<int>(__float_as_uint(v)), lane)));
 }
@@ -68,43 +56,15 @@ __global__ __launch_bounds__(kThreads, few_waves(DT, PACKED, R)) void attention_
     hi[r] = static_cast<int>(upto(frame_of(r)) - base);
   }
 
-  // the rows' digits: row lr % 4 of R, 16 columns per lane and step
-  v4i q[KS][3];
-  float row_scale[R];
+  // The rows (requested in front of the first tile, so that their digits are formed under its trip from memory)
+  float x[KS][16];
   {
     const int own = min(lr & 3, R - 1), t = frame_of(own);
     const float *const src = qkv + (b * a.T + t) * a.ld + (static_cast<int64_t>(h) * a.group + min(own, rows - 1) % a.group) * g.dh;
-    float x[KS][16];
-    uint32_t m = 0u;
 #pragma unroll
     for (int k = 0; k < KS; ++k)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const int c = 64 * k + 16 * lg + i;
-        x[k][i] = src[min(c, g.dh - 1)];
-        x[k][i] = c < g.dh ? x[k][i] : 0.0f;
-        m = max(m, __float_as_uint(x[k][i]) & 0x7FFFFFFFu);
-      }
-    m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 16, 64)));
-    m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 32, 64)));
-    const float top = __uint_as_float(m);    // a NaN or an infinity makes the row's scores NaN
-    const float to = kDigits / fmaxf(top, 0x1p-100f);
-    const float unit = (m > 0x7F800000u ? top : fmaxf(top, 0x1p-100f)) * (1.0f / kDigits) * a.scale_log2e * (PACKED ? 0.0625f : 1.0f);
-#pragma unroll
-    for (int r = 0; r < R; ++r) row_scale[r] = of_lane(unit, r);
-#pragma unroll
-    for (int k = 0; k < KS; ++k)
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        int nn[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) nn[i] = static_cast<int>(rintf(x[k][4 * w + i] * to));
-        int d0, d1, d2;
-        digits4(nn, d0, d1, d2);
-        q[k][0][w] = d0;
-        q[k][1][w] = d1;
-        q[k][2][w] = d2;
-      }
+      for (int i = 0; i < 16; ++i) x[k][i] = src[min(64 * k + 16 * lg + i, g.dh - 1)];
   }
 
   const uint8_t *const head = g.data + (b * g.kv_heads + h) * g.tiles * static_cast<int64_t>(g.tile_bytes);
@@ -151,6 +111,40 @@ __global__ __launch_bounds__(kThreads, few_waves(DT, PACKED, R)) void attention_
     load_keys(tile);
     load_values(tile);
   }
+  // the rows' digits: row lr % 4 of R, 16 columns per lane and step
+  v4i q[KS][3];
+  float row_scale[R];
+  {
+    uint32_t m = 0u;
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        x[k][i] = 64 * k + 16 * lg + i < g.dh ? x[k][i] : 0.0f;
+        m = max(m, __float_as_uint(x[k][i]) & 0x7FFFFFFFu);
+      }
+    m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 16, 64)));
+    m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), 32, 64)));
+    const float top = __uint_as_float(m);    // a NaN or an infinity makes the row's scores NaN
+    const float to = kDigits / fmaxf(top, 0x1p-100f);
+    const float unit = (m > 0x7F800000u ? top : fmaxf(top, 0x1p-100f)) * (1.0f / kDigits) * a.scale_log2e * (PACKED ? 0.0625f : 1.0f);
+#pragma unroll
+    for (int r = 0; r < R; ++r) row_scale[r] = of_lane(unit, r);
+#pragma unroll
+    for (int k = 0; k < KS; ++k)
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        int nn[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) nn[i] = static_cast<int>(rintf(x[k][4 * w + i] * to));
+        int d0, d1, d2;
+        digits4(nn, d0, d1, d2);
+        q[k][0][w] = d0;
+        q[k][1][w] = d1;
+        q[k][2][w] = d2;
+      }
+  }
+
   for (; i < tiles; i += step) {
     if (i + step < tiles) {   // otherwise this tile's once more: never another's memory
       slot += slot_step;
@@ -193,20 +187,18 @@ __global__ __launch_bounds__(kThreads, few_waves(DT, PACKED, R)) void attention_
       s[r] = joined(d[0], d[1], d[2]) * (row_scale[r] * ks_now);
     }
     vs = any ? vs : 0.0f;
-    const float vs_top = wave_max(vs);
+    const float vs_top = wave_max_positive(vs);
     float alpha[R], unit[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      const float mx = wave_max(see[r] ? s[r] : kLowest), mnew = fmaxf(m[r], mx);
+      const float mx = wave_max_signed(see[r] ? s[r] : kLowest), mnew = fmaxf(m[r], mx);
       alpha[r] = __builtin_amdgcn_exp2f(m[r] - mnew);
       m[r] = mnew;
       const float p = see[r] ? __builtin_amdgcn_exp2f(s[r] - mnew) : 0.0f;
       l[r] = fmaf(l[r], alpha[r], p);
       const float top = fmaxf(__builtin_amdgcn_exp2f(mx - mnew) * vs_top, 0x1p-100f);
       unit[r] = top * (1.0f / kDigits) * (PACKED ? 0.0625f : 1.0f);
-      // 2^23 + an integer of 23 bits: rounded to nearest by the sum; the digits' bytes are balanced as in digits4
-      const float x = fmaf(p, vs * (kDigits * __builtin_amdgcn_rcpf(top)), 8388608.0f);
-      const uint32_t u = (__float_as_uint(x) + 0x00808080u) ^ 0x00808080u;
+      const uint32_t u = weight_bits(p, vs * (kDigits * __builtin_amdgcn_rcpf(top))) ^ 0x00008080u;
       put[(2 * R + r) * 64] = static_cast<uint8_t>(u);
       put[(R + r) * 64] = static_cast<uint8_t>(u >> 8);
       put[r * 64] = static_cast<uint8_t>(u >> 16);

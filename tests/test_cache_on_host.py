@@ -22,9 +22,9 @@ def spliced():
     shim = ('#define AQT_ON_HOST 1\n#include "vectors_on_host.h"\n#include "aqt.h"\n'
             "inline int __builtin_amdgcn_readlane(int v, int lane) { return lane_value(v, (unsigned)lane); }\n"
             # the data-parallel primitives of a maximum over the wavefront: row_shr:n, row_bcast:15, row_bcast:31
-            "inline int __builtin_amdgcn_update_dpp(int old, int v, int ctrl, int, int, bool) {\n"
+            "inline int __builtin_amdgcn_update_dpp(int old, int v, int ctrl, int rows, int, bool) {\n"
             "  const unsigned l = threadIdx.x & 63u;\n"
-            "  const bool shift = ctrl < 0x120, on = shift ? (l & 15u) >= (unsigned)(ctrl & 15) : ctrl == 0x142 ? l >= 16u : l >= 32u;\n"
+            "  const bool shift = ctrl < 0x120, on = (rows >> (l >> 4) & 1) && (shift ? (l & 15u) >= (unsigned)(ctrl & 15) : ctrl == 0x142 ? l >= 16u : l >= 32u);\n"
             "  const int from = lane_value(v, on ? (shift ? l - (unsigned)(ctrl & 15) : ctrl == 0x142 ? (l & 48u) - 1u : 31u) : l);\n"
             "  return on ? from : old;\n}\n"
             "inline float __builtin_amdgcn_rsqf(float x) { return 1.0f / sqrtf(x); }\n"
@@ -34,7 +34,8 @@ def spliced():
     return (shim + helpers + layout + read("quant_code.h") + kernels("cache.hip", "cache_", "}  // namespace\n\nbool cache_shape_ok") +
             shared + kernels("attention_cached_few.hip", "few", "template <int DT, bool PACKED>\naqt_status launch_rows").replace(
                 "typedef int key_piece __attribute__((ext_vector_type(KEYS)));", "typedef typename key_piece_of<KEYS>::type key_piece;") +
-            kernels("attention_cached.hip", "attend", "// How a call is cut up: rows of a workgroup") +
+            kernels("attention_cached.hip", "attend", "// How a call is cut up: rows of a workgroup").replace(
+                "typedef int key_piece __attribute__((ext_vector_type(KEYS)));", "typedef typename key_piece_of<KEYS>::type key_piece;") +
             kernels("rotate.hip", "turn", "__global__ void rotation_turns_kernel") +
             open(os.path.join(HERE, "host_emulation", "cache_driver.cpp")).read())
 
