@@ -220,8 +220,12 @@ def _ptr(t: Optional[torch.Tensor]):
     return None if t is None else ctypes.c_void_p(t.data_ptr())
 
 
+# the current stream's handle; the public way to it builds a Stream object, a third of a short call's time on the host
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+
+
 def _stream():
-    return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+    return ctypes.c_void_p(_raw_stream(torch.cuda.current_device()))
 
 
 def _check(status: int, where: str):
@@ -879,18 +883,19 @@ def aqt_conformer_layer_bwd(dy, x, weights: dict, saved: LayerSaved, *, B: int, 
     return dx, grads
 
 
-def _shaped(t: Optional[torch.Tensor], dtype, shape, device, name: str):
-    """A contiguous device tensor of exactly that type and shape, on the device the call runs on (None passes)."""
-    if t is not None and not (t.dtype == dtype and tuple(t.shape) == tuple(shape) and t.is_contiguous() and t.device == device):
-        raise TypeError(f"{name}: expected a contiguous {dtype} tensor {tuple(shape)} on {device}")
+def _shaped(t: Optional[torch.Tensor], dtype, shape: tuple, device: int, name: str):
+    """A contiguous tensor of exactly that type and shape on that device (None passes)."""
+    if t is not None and (t.dtype is not dtype or t.shape != shape or t.get_device() != device or not t.is_contiguous()):
+        raise TypeError(f"{name}: expected a contiguous {dtype} tensor {shape} on device {device}")
     return t
 
 
-def _current(t: torch.Tensor, name: str):
-    """The launches go to the current device's current stream."""
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+def _current(t: torch.Tensor, name: str) -> int:
+    """The index of the device that the tensor is on: the current one, whose current stream takes the launches."""
+    device = t.get_device()
+    if device < 0 or device != torch.cuda.current_device():
         raise ValueError(f"{name}: expected a tensor on the current device")
-    return t.device
+    return device
 
 
 class QkNormRotate:
@@ -907,9 +912,9 @@ class QkNormRotate:
         self.gamma_q, self.gamma_k = gamma_q, gamma_k
         for name, t in (("gamma_q", gamma_q), ("gamma_k", gamma_k)):
             if t is not None:
-                _shaped(_dev(t, torch.float32, name), torch.float32, (dh,), t.device, name)
+                _shaped(t, torch.float32, (dh,), _current(t, name), name)
         if turns is not None:
-            _shaped(_dev(turns, torch.float64, "turns"), torch.float64, (rot // 2,), turns.device, "turns")
+            _shaped(turns, torch.float64, (rot // 2,), _current(turns, "turns"), "turns")
         elif rot:
             turns = torch.empty(max(rot // 2, 1), dtype=torch.float64, device=device)
             _check(lib().aqt_rotation_turns(rot, base, _ptr(turns), _stream()), "aqt_rotation_turns")
@@ -917,6 +922,7 @@ class QkNormRotate:
         self.c = aqt_qk_norm_rotate(heads, kv_heads, dh, int(self.norm), eps, rot, pairing,
                                     None if gamma_q is None else gamma_q.data_ptr(), None if gamma_k is None else gamma_k.data_ptr(),
                                     None if turns is None else turns.data_ptr())
+        self.ref = ctypes.byref(self.c)
 
 
 def aqt_qk_norm_rotate_fwd(qkv, B: int, T: int, spec: QkNormRotate, *, first=None, out=None):
@@ -926,8 +932,8 @@ def aqt_qk_norm_rotate_fwd(qkv, B: int, T: int, spec: QkNormRotate, *, first=Non
     _shaped(qkv, torch.float32, (B * T, spec.columns), dev, "qkv")
     _shaped(first, torch.int64, (B,), dev, "first")
     out = torch.empty_like(qkv) if out is None else _shaped(out, torch.float32, qkv.shape, dev, "out")
-    _check(lib().aqt_qk_norm_rotate_fwd(qkv.data_ptr(), B, T, ctypes.byref(spec.c), None if first is None else first.data_ptr(),
-                                        out.data_ptr(), _stream()), "aqt_qk_norm_rotate_fwd")
+    _check(lib().aqt_qk_norm_rotate_fwd(qkv.data_ptr(), B, T, spec.ref, None if first is None else first.data_ptr(),
+                                        out.data_ptr(), _raw_stream(dev)), "aqt_qk_norm_rotate_fwd")
     return out
 
 
@@ -941,11 +947,11 @@ def aqt_qk_norm_rotate_bwd(qkv, dout, B: int, T: int, spec: QkNormRotate, *, fir
     dqkv = torch.empty_like(dout) if dqkv is None else _shaped(dqkv, torch.float32, dout.shape, dev, "dqkv")
     dq = dk = None
     if want_gamma and spec.norm:
-        dq, dk = (torch.empty(spec.dh, dtype=torch.float32, device=dev) for _ in range(2))
+        dq, dk = (torch.empty(spec.dh, dtype=torch.float32, device=dout.device) for _ in range(2))
         ws = workspace(aqt_workspace_bytes(AQT_OP_QK_NORM_ROTATE_BWD, B * T, spec.dh, 1), dev) if ws is None else ws
-    _check(lib().aqt_qk_norm_rotate_bwd(None if qkv is None else qkv.data_ptr(), dout.data_ptr(), B, T, ctypes.byref(spec.c),
+    _check(lib().aqt_qk_norm_rotate_bwd(None if qkv is None else qkv.data_ptr(), dout.data_ptr(), B, T, spec.ref,
                                         None if first is None else first.data_ptr(), dqkv.data_ptr(), _ptr(dq), _ptr(dk), _ptr(ws),
-                                        0 if ws is None else ws.numel(), _stream()), "aqt_qk_norm_rotate_bwd")
+                                        0 if ws is None else ws.numel(), _raw_stream(dev)), "aqt_qk_norm_rotate_bwd")
     return dqkv, dq, dk
 
 
@@ -956,19 +962,20 @@ class KvCache:
     def __init__(self, streams: int, capacity: int, kv_heads: int, dh: int, bits: int = 8, *, length=None, device="cuda"):
         self.streams, self.capacity, self.kv_heads, self.dh, self.bits = streams, capacity, kv_heads, dh, bits
         self.c = aqt_cache(streams, capacity, kv_heads, dh, bits, None, None)
-        nbytes = int(lib().aqt_cache_bytes(ctypes.byref(self.c)))
+        self.ref = ctypes.byref(self.c)
+        nbytes = int(lib().aqt_cache_bytes(self.ref))
         if nbytes == 0:
             raise AqtError(AQT_ERR_INVALID_ARG, "aqt_cache_bytes")
         self.data = torch.empty(nbytes, dtype=torch.uint8, device=device)
         self.length = torch.zeros(streams, dtype=torch.int64, device=device) if length is None else length
-        _shaped(self.length, torch.int64, (streams,), self.data.device, "length")
+        _shaped(self.length, torch.int64, (streams,), self.data.get_device(), "length")
         self.c.data, self.c.length = self.data.data_ptr(), self.length.data_ptr()
 
     def advance(self, T: int, count=None):
         """aqt_cache_advance: the streams have T (or count[b]) frames more; after the last layer of a step."""
         dev = _current(self.length, "length")
         _shaped(count, torch.int32, (self.streams,), dev, "count")
-        _check(lib().aqt_cache_advance(_ptr(self.length), self.streams, T, _ptr(count), _stream()), "aqt_cache_advance")
+        _check(lib().aqt_cache_advance(_ptr(self.length), self.streams, T, _ptr(count), _raw_stream(dev)), "aqt_cache_advance")
         return self
 
 
@@ -976,7 +983,7 @@ def _new_rows(qkv, cache: KvCache, T: int, heads: int, count):
     dev = _current(qkv, "qkv")
     _shaped(qkv, torch.float32, (cache.streams * T, (heads + 2 * cache.kv_heads) * cache.dh), dev, "qkv")
     _shaped(count, torch.int32, (cache.streams,), dev, "count")
-    if cache.data.device != dev:
+    if cache.data.get_device() != dev:
         raise ValueError("cache: expected a cache on the current device")
     return dev
 
@@ -984,8 +991,8 @@ def _new_rows(qkv, cache: KvCache, T: int, heads: int, count):
 def aqt_cache_append(qkv, cache: KvCache, T: int, heads: int, *, count=None, dev_status=None):
     """aqt_cache_append: quantize the keys and values of qkv [streams*T, (heads + 2 kv_heads) dh] into the cache, behind the
     frames that cache.length names.  count: int32 [streams], how many of the T frames each stream brings."""
-    _new_rows(qkv, cache, T, heads, count)
-    _check(lib().aqt_cache_append(qkv.data_ptr(), T, heads, ctypes.byref(cache.c), None if count is None else count.data_ptr(), _stream(),
+    dev = _new_rows(qkv, cache, T, heads, count)
+    _check(lib().aqt_cache_append(qkv.data_ptr(), T, heads, cache.ref, None if count is None else count.data_ptr(), _raw_stream(dev),
                                   None if dev_status is None else dev_status.data_ptr()), "aqt_cache_append")
 
 
@@ -998,17 +1005,17 @@ def aqt_cache_read(cache: KvCache, n: int, *, first=None, pending: int = 0, coun
     _shaped(first, torch.int64, (cache.streams,), dev, "first")
     _shaped(count, torch.int32, (cache.streams,), dev, "count")
     if want_keys:
-        keys = torch.empty(shape, dtype=torch.float32, device=dev) if keys is None else _shaped(keys, torch.float32, shape, dev, "keys")
+        keys = torch.empty(shape, dtype=torch.float32, device=cache.data.device) if keys is None else _shaped(keys, torch.float32, shape, dev, "keys")
     if want_values:
-        values = torch.empty(shape, dtype=torch.float32, device=dev) if values is None else _shaped(values, torch.float32, shape, dev, "values")
+        values = torch.empty(shape, dtype=torch.float32, device=cache.data.device) if values is None else _shaped(values, torch.float32, shape, dev, "values")
     keys, values = keys if want_keys else None, values if want_values else None
-    _check(lib().aqt_cache_read(ctypes.byref(cache.c), pending, None if count is None else count.data_ptr(),
-                                None if first is None else first.data_ptr(), n, _ptr(keys), _ptr(values), _stream()), "aqt_cache_read")
+    _check(lib().aqt_cache_read(cache.ref, pending, None if count is None else count.data_ptr(),
+                                None if first is None else first.data_ptr(), n, _ptr(keys), _ptr(values), _raw_stream(dev)), "aqt_cache_read")
     return keys, values
 
 
 def aqt_attention_cached_workspace_bytes(cache: KvCache, T: int, heads: int) -> int:
-    return int(lib().aqt_attention_cached_workspace_bytes(ctypes.byref(cache.c), T, heads))
+    return int(lib().aqt_attention_cached_workspace_bytes(cache.ref, T, heads))
 
 
 def aqt_attention_cached_fwd(qkv, cache: KvCache, T: int, heads: int, *, left: int = -1, right: int = 0, count=None, ctx=None,
@@ -1018,12 +1025,12 @@ def aqt_attention_cached_fwd(qkv, cache: KvCache, T: int, heads: int, *, left: i
     dev = _new_rows(qkv, cache, T, heads, count)
     shape = (cache.streams * T, heads * cache.dh)
     if ctx is None:
-        ctx = (torch.empty if count is None else torch.zeros)(shape, dtype=torch.float32, device=dev)
+        ctx = (torch.empty if count is None else torch.zeros)(shape, dtype=torch.float32, device=qkv.device)
     else:
         _shaped(ctx, torch.float32, shape, dev, "ctx")
-    m = torch.empty(1, dtype=torch.float32, device=dev) if want_absmax else None
+    m = torch.empty(1, dtype=torch.float32, device=qkv.device) if want_absmax else None
     ws = workspace(aqt_attention_cached_workspace_bytes(cache, T, heads), dev) if ws is None else ws
-    _check(lib().aqt_attention_cached_fwd(qkv.data_ptr(), T, heads, ctypes.byref(cache.c), None if count is None else count.data_ptr(),
+    _check(lib().aqt_attention_cached_fwd(qkv.data_ptr(), T, heads, cache.ref, None if count is None else count.data_ptr(),
                                           left, right, ctx.data_ptr(), None if m is None else m.data_ptr(), ws.data_ptr(), ws.numel(),
-                                          _stream()), "aqt_attention_cached_fwd")
+                                          _raw_stream(dev)), "aqt_attention_cached_fwd")
     return ctx, m

@@ -406,6 +406,8 @@ __global__ void zero_word_kernel(uint32_t *p) {
 
 int cols_of(int dh) { return dh <= 32 ? 32 : dh <= 64 ? 64 : 128; }
 
+constexpr int64_t kSplitTiles = 24;
+
 // How a call is cut up: rows of a workgroup (all that share a key / value head, where they are few), row tiles, and the workgroups
 // (splits) that share the tiles of a row tile: a tile for every wavefront at most.
 struct CachedCut {
@@ -423,7 +425,9 @@ CachedCut cut_of(const CacheGeom &g, int64_t rows, int64_t window) {
   // and request its first tile while the others work (32 streams, four rows of 128 columns: 108 us with 512 workgroups, 113 with
   // 1024, 123 with 2048; 8 streams of 128 rows: 64 us with 512, 67 with 1024, 74 with 2048).
   const int64_t want = 256 * (c.rows <= kFewRows ? few_waves(dt, g.packed, c.rows) : many_waves(dt, g.packed)) / c.groups;
-  const int64_t most = cdiv(cdiv(window, 64) + 1, kWaves), s = want < most ? want : most;
+  // A split has its price, the second launch: under kSplitTiles it takes longer than the tiles that it saves (32 streams of 16 frames with a
+  // window of 5 tiles: 11.1 us in two splits, 8.8 in one), and a wavefront gets two tiles at least.
+  const int64_t tiles = cdiv(window, 64) + 1, most = tiles < kSplitTiles ? 1 : tiles / (2 * kWaves), s = want < most ? want : most;
   c.splits = static_cast<int>(s < 1 ? 1 : s);
   return c;
 }

@@ -27,6 +27,26 @@ __device__ __forceinline__ void transpose_bytes(uint32_t (&w)[4]) {
   w[3] = __builtin_amdgcn_perm(cd1, ab1, 0x07060302u);
 }
 
+// Four codes, the first in the lowest byte.  r is 1 / s to 2^-23 of it: then x r is within 2^-14 of x / s, and where it lies no nearer than 2^-13
+// to the middle between two whole numbers its nearest one is the floor that defines the code; otherwise (one quad in a thousand)
+// the four are divided.  x r + 1.5 2^23 rounds to that whole number, in its lowest bits.  No value exceeds its group's maximum, so no
+// code is clamped.  r is 0 where s is no ordinary number.
+__device__ __forceinline__ uint32_t codes4(const float (&x)[4], float s, float r, float fq) {
+  constexpr float kWhole = 12582912.0f;
+  uint32_t n[4];
+  float off[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const float w = fmaf(x[e], r, kWhole);
+    n[e] = __float_as_uint(w);
+    off[e] = fabsf(fmaf(x[e], r, kWhole - w));
+  }
+  if (r == 0.0f || !(fmaxf(fmaxf(off[0], off[1]), fmaxf(off[2], off[3])) < 0.5f - 0x1p-13f))
+    return quant4_divided(x[0], x[1], x[2], x[3], Quantizer{s, fq, 0.0f, false});
+  const uint32_t lo = __builtin_amdgcn_perm(n[1], n[0], 0x0C0C0400u), hi = __builtin_amdgcn_perm(n[3], n[2], 0x0C0C0400u);
+  return __builtin_amdgcn_perm(hi, lo, 0x05040100u);
+}
+
 // What a group of lanes works on: four frames from `frame` (a multiple of four, possibly negative) of head h.
 struct Quad {
   int64_t frame;
@@ -122,9 +142,9 @@ __global__ __launch_bounds__(kThreadsMax) void cache_append_kernel(const float *
 #pragma unroll
     for (int off = 1; off < L; off <<= 1) m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), off, 64)));
     const float fq = static_cast<float>(g.qmax), s = __uint_as_float(m) / fq;
-    const Quantizer k = quantizer(s, fq);
+    const float r = s > 0x1p-60f && s < 0x1p60f ? __builtin_amdgcn_rcpf(s) : 0.0f;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) code[h][i] = quant4(x[i][h][0], x[i][h][1], x[i][h][2], x[i][h][3], k);
+    for (int h = 0; h < 2; ++h) code[h][i] = codes4(x[i][h], s, r, fq);
     if (j == 0 && mine[i]) {
       reinterpret_cast<float *>(tile + cache_scales(g))[(q.values ? 64 : 0) + key + i] = s;
       if (dev_status && m >= 0x7F800000u) *dev_status = AQT_ERR_NONFINITE;

@@ -34,7 +34,7 @@ def spliced():
     return (shim + helpers + layout + read("quant_code.h") + kernels("cache.hip", "cache_", "}  // namespace\n\nbool cache_shape_ok") +
             shared + kernels("attention_cached_few.hip", "few", "template <int DT, bool PACKED>\naqt_status launch_rows").replace(
                 "typedef int key_piece __attribute__((ext_vector_type(KEYS)));", "typedef typename key_piece_of<KEYS>::type key_piece;") +
-            kernels("attention_cached.hip", "attend", "// How a call is cut up: rows of a workgroup").replace(
+            kernels("attention_cached.hip", "attend", "constexpr int64_t kSplitTiles").replace(
                 "typedef int key_piece __attribute__((ext_vector_type(KEYS)));", "typedef typename key_piece_of<KEYS>::type key_piece;") +
             kernels("rotate.hip", "turn", "__global__ void rotation_turns_kernel") +
             open(os.path.join(HERE, "host_emulation", "cache_driver.cpp")).read())
