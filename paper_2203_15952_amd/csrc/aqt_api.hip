@@ -511,7 +511,7 @@ aqt_status rotate_check(int64_t B, int64_t T, const aqt_qk_norm_rotate *s) {
   if (s->rot < 0 || s->rot % 2 || s->rot > s->dh || (s->rot && !s->turns) || !(s->eps >= 0.0f)) return AQT_ERR_INVALID_ARG;
   if (s->pairing != AQT_ROTATE_HALVES && s->pairing != AQT_ROTATE_PAIRS) return AQT_ERR_INVALID_ARG;
   if (s->dh > 128 || s->heads > (1 << 20)) return AQT_ERR_UNSUPPORTED;
-  return T <= (int64_t(1) << 50) / B ? AQT_OK : AQT_ERR_UNSUPPORTED;   // (2^50 rows: the rest is the tensor's own limit)
+  return T <= (int64_t(1) << 60) / static_cast<int64_t>(rotate_row_bytes(*s)) / B ? AQT_OK : AQT_ERR_UNSUPPORTED;   // bytes count in 64 bits
 }
 
 aqt_status cache_check(const aqt_cache *c) {

@@ -304,8 +304,10 @@ bool grid_ok(const CacheGeom &g, int64_t n) {
 }  // namespace
 
 bool cache_shape_ok(const aqt_cache &c) {
-  return c.streams >= 1 && c.capacity >= 64 && c.capacity % 64 == 0 && c.capacity / 64 <= (1 << 24) && c.kv_heads >= 1 &&
-         c.kv_heads <= 4096 && c.dh >= 1 && c.dh <= 128 && bits_ok(c.bits) && c.streams <= (int64_t(1) << 24);
+  const int64_t tiles = c.capacity / 64;
+  return c.streams >= 1 && c.capacity >= 64 && c.capacity % 64 == 0 && tiles <= (1 << 24) && c.kv_heads >= 1 && c.kv_heads <= 4096 &&
+         c.dh >= 1 && c.dh <= 128 && bits_ok(c.bits) && c.streams <= (int64_t(1) << 24) &&
+         c.streams * c.kv_heads <= (int64_t(1) << 46) / tiles;   // a tile takes 17 KB at most: bytes count in 64 bits
 }
 
 CacheGeom cache_geom(const aqt_cache &c) {

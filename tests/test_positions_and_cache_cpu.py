@@ -44,6 +44,7 @@ def test_rotation_refuses_arguments(L):
     assert fwd(None, 2, 3, spec(), None, BIG, None) == INVALID and fwd(ONE, 2, 3, spec(), None, None, None) == INVALID
     assert fwd(ONE, 0, 3, spec(), None, BIG, None) == INVALID and fwd(ONE, 2, 0, spec(), None, BIG, None) == INVALID
     assert fwd(ONE, 1 << 40, 1 << 40, spec(), None, BIG, None) == UNSUPPORTED
+    assert fwd(ONE, 1 << 30, 1 << 21, spec(heads=1 << 20, kv_heads=1 << 20), None, BIG, None) == UNSUPPORTED
     assert fwd(ONE, 2, 3, spec(), None, ONE + 64, None) == INVALID            # overlaps, but is not, the input
     need = B.aqt_workspace_bytes(B.AQT_OP_QK_NORM_ROTATE_BWD, 6, 16, 1)
     assert need >= 2 * 16 * 4 and B.aqt_workspace_bytes(B.AQT_OP_QK_NORM_ROTATE_BWD, 6, 129, 1) == 0
@@ -62,7 +63,8 @@ def test_rotation_refuses_arguments(L):
 
 BAD_CACHES = [(dict(streams=0), INVALID), (dict(capacity=0), INVALID), (dict(capacity=100), INVALID), (dict(capacity=-64), INVALID),
               (dict(kv_heads=0), INVALID), (dict(dh=0), INVALID), (dict(dh=129), UNSUPPORTED), (dict(bits=1), UNSUPPORTED),
-              (dict(bits=9), UNSUPPORTED), (dict(streams=1 << 25), UNSUPPORTED), (dict(capacity=1 << 32), UNSUPPORTED)]
+              (dict(bits=9), UNSUPPORTED), (dict(streams=1 << 25), UNSUPPORTED), (dict(capacity=1 << 32), UNSUPPORTED),
+              (dict(streams=1 << 24, capacity=1 << 24, kv_heads=4096), UNSUPPORTED)]
 
 
 @pytest.mark.parametrize("kw,status", BAD_CACHES)
