@@ -329,12 +329,9 @@ __global__ __launch_bounds__(kThreads) void attention_cached_join_kernel(const f
   __shared__ __attribute__((aligned(16))) float so[N][N == 1 ? 4 : ROWS * COLS];
   __shared__ float sm[N][ROWS], sl[N][ROWS];
   const int tid = static_cast<int>(threadIdx.x), slice = SLICES == 1 ? 0 : tid / QUADS;
-  int64_t id = blockIdx.x;
-  const float *const from = part + id * a.splits * P::kFloats;
-  const int rt = static_cast<int>(id % a.row_tiles);
-  id /= a.row_tiles;
-  const int h = static_cast<int>(id % g.kv_heads);
-  const int64_t b = id / g.kv_heads;
+  const int id = static_cast<int>(blockIdx.x), rt = id % a.row_tiles, bh = id / a.row_tiles, h = bh % g.kv_heads;
+  const float *const from = part + static_cast<int64_t>(id) * a.splits * P::kFloats;
+  const int64_t b = bh / g.kv_heads;
   const StreamFrames f = stream_frames(g, count, a.T, b);
   const int n = static_cast<int>(f.end - f.length);
   uint32_t amax = 0u;                     // (parts of frames that the stream did not bring were not written, and are not stored)

@@ -110,13 +110,14 @@ static void one(int streams, int64_t capacity, int heads, int kv, int dh, int bi
     free(first); free(rk); free(rv);
     // attention of the new frames
     for (auto [left, right] : windows) {
+      if (T > 32 && left != windows[0].first) continue;
       CachedGeom a{};
       a.T = T; a.ld = cols; a.heads = heads; a.group = group;
       a.left = left; a.right = right; a.scale_log2e = (float)(1.4426950408889634 / sqrt((double)dh));
       // in tiles of 16 rows, and where they are few, each in its own place; by itself, and joined from three parts
       for (int form = 0; form < 4; ++form) {
         const int few_rows = T * group <= kFewRows ? (T * group == 1 ? 1 : T * group == 2 ? 2 : 4) : 0, rows = form & 2 ? few_rows : 16;
-        if (rows == 0) continue;
+        if (rows == 0 || (T > 32 && form == 0)) continue;
         a.splits = form & 1 ? 3 : 1;
         a.row_tiles = (T * group + rows - 1) / rows;
         const int groups = streams * kv * a.row_tiles, COLS = attend::cols_of(dh), splits = a.splits;
@@ -197,6 +198,7 @@ static void rotate_case(int64_t B, int64_t T, int heads, int kv, int dh, int rot
   g.turns = np ? turns : nullptr; g.first = first ? f0 : nullptr; g.gamma[0] = gains ? gq : nullptr; g.gamma[1] = gains ? gk : nullptr;
   const bool can = dh % 4 == 0 && (!halves || rot % 8 == 0);
   for (int pieces = can; pieces >= 0; --pieces) for (int blocks : {1, 3}) {
+    if (blocks == 1 && dh != 36) continue;
     float *part = floats((size_t)blocks * 2 * dh);
     if (halves) { turn_paired<true, false>(x, nullptr, g, out, nullptr, pieces, blocks); turn_paired<true, true>(norm ? x : nullptr, dy, g, dx, part, pieces, blocks); }
     else { turn_paired<false, false>(x, nullptr, g, out, nullptr, pieces, blocks); turn_paired<false, true>(norm ? x : nullptr, dy, g, dx, part, pieces, blocks); }
@@ -255,13 +257,13 @@ int main(int argc, char **) {
     rotate_case(1, 40, 2, 1, 8, 8, false, true, true, true, false);
     rotate_case(1, 2, 2, 2, 101, 100, true, true, true, true, false);
   } else {
-    one(3, 64, 1, 1, 64, 8, {5, 62, 1, 70}, {{-1, 0}, {7, 3}}, true);
-    one(1, 128, 4, 2, 36, 4, {17, 120, 4}, {{-1, -1}, {0, 0}}, false);
+    one(2, 64, 1, 1, 64, 8, {5, 62, 1, 70}, {{-1, 0}, {7, 3}}, true);
+    one(1, 128, 2, 1, 36, 4, {17, 115, 2}, {{-1, -1}, {0, 0}}, false);
     one(1, 64, 6, 1, 128, 4, {3, 1}, {{2, 0}, {-1, 2}}, false);
     one(2, 64, 1, 1, 5, 6, {4, 66, 3}, {{-1, 0}}, true);
-    one(1, 128, 1, 1, 80, 3, {60, 100}, {{30, 1}}, false);
+    one(1, 128, 1, 1, 80, 3, {60, 90}, {{30, 1}}, false);
     one(1, 64, 2, 1, 128, 8, {9, 1}, {{-1, 0}}, false);
-    one(2, 64, 40, 2, 16, 2, {3, 1}, {{-1, 0}, {1, 1}}, true);
+    one(2, 64, 20, 1, 16, 2, {3, 1}, {{-1, 0}, {1, 1}}, true);
   }
   printf(bad ? "MISMATCH\n" : "ok\n");
   return bad;

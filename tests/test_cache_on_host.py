@@ -44,7 +44,7 @@ def spliced():
 def exe(tmp_path_factory):
     path = tmp_path_factory.mktemp("cache_on_host")
     (path / "cache.cpp").write_text(spliced())
-    r = subprocess.run(["g++", "-O1", "-g", "-fsanitize=address,undefined", "-fno-sanitize-recover=all", "-static-libasan", "-static-libubsan",
+    r = subprocess.run(["g++", "-O0", "-g1", "-fsanitize=address,undefined", "-fno-sanitize-recover=all", "-static-libasan", "-static-libubsan",
                         "-std=c++20", "-pthread", "-I", os.path.join(HERE, "host_emulation"), "-I", os.path.join(ROOT, "include"),
                         str(path / "cache.cpp"), "-o", str(path / "cache")], capture_output=True, text=True)
     assert r.returncode == 0, r.stderr[-3000:]

@@ -266,6 +266,34 @@ def test_attention_over_the_cache(shape, steps, window, scale, ragged):
         cache.advance(T, cd)
 
 
+@pytest.mark.parametrize("T,group", [(3, 1), (24, 1), (2, 4)])
+def test_a_cache_beyond_4_gib(T, group):
+    """The last head's tiles lie behind byte 2^32 of the buffer, the ring's end too."""
+    kv, dh, capacity = 4, 64, 1 << 23
+    say("large cache", T, group)
+    heads = kv * group
+    cache = B.KvCache(1, capacity, kv, dh, 8)
+    assert cache.data.numel() > 1 << 32
+    ref = Streams(1, capacity, heads, kv, dh, 8)
+    ref.base[:] = 3 * capacity - 70
+    cache.length.fill_(int(ref.base[0]))
+    rng = np.random.default_rng(T)
+    for n in (60, T):          # across the end of the ring
+        rows = new_rows(rng, 1, n, ref.cols)
+        B.aqt_cache_append(dev(rows), cache, n, heads)
+        ref.append(rows, n)
+        if n == 60:
+            cache.advance(n)
+    length = host(cache.length)
+    ctx, _ = B.aqt_attention_cached_fwd(dev(rows), cache, T, heads, left=40, right=0)
+    want, tol = ref.attention(rows, T, length, None, 40, 0, np.zeros((T, heads * dh)))
+    np.testing.assert_array_less(np.abs(host(ctx) - want), tol + 1e-30)
+    keys, values = B.aqt_cache_read(cache, 50, pending=T)
+    first = ref.end(0) - 50
+    np.testing.assert_array_equal(host(keys).reshape(50, kv, dh), ref.frames("k", 0, first, 50))
+    np.testing.assert_array_equal(host(values).reshape(50, kv, dh), ref.frames("v", 0, first, 50))
+
+
 def test_rows_that_see_nothing_are_zeros():
     """More new frames than the cache holds: the first ones' windows lie before its oldest frame."""
     cache, ref = make(1, 64, 2, 1, 32, 8)
