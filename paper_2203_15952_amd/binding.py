@@ -898,6 +898,12 @@ def _current(t: torch.Tensor, name: str) -> int:
     return device
 
 
+def _space(ws: torch.Tensor, device: int) -> torch.Tensor:
+    if ws.dtype is not torch.uint8 or ws.get_device() != device or not ws.is_contiguous():
+        raise TypeError(f"ws: expected a contiguous uint8 tensor on device {device}")
+    return ws
+
+
 class QkNormRotate:
     """How queries and keys of rows with `heads` queries, `kv_heads` keys and values of dh columns are normalised and rotated
     (aqt_qk_norm_rotate_fwd / _bwd), and its aqt_qk_norm_rotate view.  rot: leading columns of a head that are rotated (default:
@@ -917,12 +923,19 @@ class QkNormRotate:
             _shaped(turns, torch.float64, (rot // 2,), _current(turns, "turns"), "turns")
         elif rot:
             turns = torch.empty(max(rot // 2, 1), dtype=torch.float64, device=device)
+            _current(turns, "device")
             _check(lib().aqt_rotation_turns(rot, base, _ptr(turns), _stream()), "aqt_rotation_turns")
         self.turns = turns
+        self.device = next((t.get_device() for t in (turns, gamma_q, gamma_k) if t is not None), None)   # all on the current one
         self.c = aqt_qk_norm_rotate(heads, kv_heads, dh, int(self.norm), eps, rot, pairing,
                                     None if gamma_q is None else gamma_q.data_ptr(), None if gamma_k is None else gamma_k.data_ptr(),
                                     None if turns is None else turns.data_ptr())
         self.ref = ctypes.byref(self.c)
+
+    def on(self, device: int):
+        if self.device is not None and self.device != device:
+            raise ValueError("spec: expected gains and turns on the current device")
+        return self.ref
 
 
 def aqt_qk_norm_rotate_fwd(qkv, B: int, T: int, spec: QkNormRotate, *, first=None, out=None):
@@ -932,7 +945,7 @@ def aqt_qk_norm_rotate_fwd(qkv, B: int, T: int, spec: QkNormRotate, *, first=Non
     _shaped(qkv, torch.float32, (B * T, spec.columns), dev, "qkv")
     _shaped(first, torch.int64, (B,), dev, "first")
     out = torch.empty_like(qkv) if out is None else _shaped(out, torch.float32, qkv.shape, dev, "out")
-    _check(lib().aqt_qk_norm_rotate_fwd(qkv.data_ptr(), B, T, spec.ref, None if first is None else first.data_ptr(),
+    _check(lib().aqt_qk_norm_rotate_fwd(qkv.data_ptr(), B, T, spec.on(dev), None if first is None else first.data_ptr(),
                                         out.data_ptr(), _raw_stream(dev)), "aqt_qk_norm_rotate_fwd")
     return out
 
@@ -948,8 +961,8 @@ def aqt_qk_norm_rotate_bwd(qkv, dout, B: int, T: int, spec: QkNormRotate, *, fir
     dq = dk = None
     if want_gamma and spec.norm:
         dq, dk = (torch.empty(spec.dh, dtype=torch.float32, device=dout.device) for _ in range(2))
-        ws = workspace(aqt_workspace_bytes(AQT_OP_QK_NORM_ROTATE_BWD, B * T, spec.dh, 1), dev) if ws is None else ws
-    _check(lib().aqt_qk_norm_rotate_bwd(None if qkv is None else qkv.data_ptr(), dout.data_ptr(), B, T, spec.ref,
+        ws = workspace(aqt_workspace_bytes(AQT_OP_QK_NORM_ROTATE_BWD, B * T, spec.dh, 1), dev) if ws is None else _space(ws, dev)
+    _check(lib().aqt_qk_norm_rotate_bwd(None if qkv is None else qkv.data_ptr(), dout.data_ptr(), B, T, spec.on(dev),
                                         None if first is None else first.data_ptr(), dqkv.data_ptr(), _ptr(dq), _ptr(dk), _ptr(ws),
                                         0 if ws is None else ws.numel(), _raw_stream(dev)), "aqt_qk_norm_rotate_bwd")
     return dqkv, dq, dk
@@ -957,7 +970,8 @@ def aqt_qk_norm_rotate_bwd(qkv, dout, B: int, T: int, spec: QkNormRotate, *, fir
 
 class KvCache:
     """A quantized cache of keys and values (aqt_cache_append, aqt_cache_read, aqt_attention_cached_fwd): its buffer, the streams'
-    lengths (int64 [streams], zeros unless given: the caches of all layers of a model share one) and its aqt_cache view."""
+    lengths (int64 [streams], zeros unless given: the caches of all layers of a model share one) and its aqt_cache view.  The
+    lengths are changed in place (a stream begins anew at length[b] = 0), never by another tensor in their place."""
 
     def __init__(self, streams: int, capacity: int, kv_heads: int, dh: int, bits: int = 8, *, length=None, device="cuda"):
         self.streams, self.capacity, self.kv_heads, self.dh, self.bits = streams, capacity, kv_heads, dh, bits
@@ -966,10 +980,19 @@ class KvCache:
         nbytes = int(lib().aqt_cache_bytes(self.ref))
         if nbytes == 0:
             raise AqtError(AQT_ERR_INVALID_ARG, "aqt_cache_bytes")
-        self.data = torch.empty(nbytes, dtype=torch.uint8, device=device)
-        self.length = torch.zeros(streams, dtype=torch.int64, device=device) if length is None else length
-        _shaped(self.length, torch.int64, (streams,), self.data.get_device(), "length")
-        self.c.data, self.c.length = self.data.data_ptr(), self.length.data_ptr()
+        self._data = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        self._length = torch.zeros(streams, dtype=torch.int64, device=device) if length is None else length
+        self._device = self._data.get_device()
+        _shaped(self._length, torch.int64, (streams,), self._device, "length")
+        self.c.data, self.c.length = self._data.data_ptr(), self._length.data_ptr()
+
+    @property
+    def data(self) -> torch.Tensor:
+        return self._data
+
+    @property
+    def length(self) -> torch.Tensor:
+        return self._length
 
     def advance(self, T: int, count=None):
         """aqt_cache_advance: the streams have T (or count[b]) frames more; after the last layer of a step."""
@@ -983,7 +1006,7 @@ def _new_rows(qkv, cache: KvCache, T: int, heads: int, count):
     dev = _current(qkv, "qkv")
     _shaped(qkv, torch.float32, (cache.streams * T, (heads + 2 * cache.kv_heads) * cache.dh), dev, "qkv")
     _shaped(count, torch.int32, (cache.streams,), dev, "count")
-    if cache.data.get_device() != dev:
+    if cache._device != dev:
         raise ValueError("cache: expected a cache on the current device")
     return dev
 
@@ -992,6 +1015,7 @@ def aqt_cache_append(qkv, cache: KvCache, T: int, heads: int, *, count=None, dev
     """aqt_cache_append: quantize the keys and values of qkv [streams*T, (heads + 2 kv_heads) dh] into the cache, behind the
     frames that cache.length names.  count: int32 [streams], how many of the T frames each stream brings."""
     dev = _new_rows(qkv, cache, T, heads, count)
+    _shaped(dev_status, torch.int32, (1,), dev, "dev_status")
     _check(lib().aqt_cache_append(qkv.data_ptr(), T, heads, cache.ref, None if count is None else count.data_ptr(), _raw_stream(dev),
                                   None if dev_status is None else dev_status.data_ptr()), "aqt_cache_append")
 
@@ -1029,7 +1053,7 @@ def aqt_attention_cached_fwd(qkv, cache: KvCache, T: int, heads: int, *, left: i
     else:
         _shaped(ctx, torch.float32, shape, dev, "ctx")
     m = torch.empty(1, dtype=torch.float32, device=qkv.device) if want_absmax else None
-    ws = workspace(aqt_attention_cached_workspace_bytes(cache, T, heads), dev) if ws is None else ws
+    ws = workspace(aqt_attention_cached_workspace_bytes(cache, T, heads), dev) if ws is None else _space(ws, dev)
     _check(lib().aqt_attention_cached_fwd(qkv.data_ptr(), T, heads, cache.ref, None if count is None else count.data_ptr(),
                                           left, right, ctx.data_ptr(), None if m is None else m.data_ptr(), ws.data_ptr(), ws.numel(),
                                           _raw_stream(dev)), "aqt_attention_cached_fwd")

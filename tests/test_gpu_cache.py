@@ -374,6 +374,12 @@ def test_binding_refuses():
         B.aqt_attention_cached_fwd(rows, cache, 3, 2, ws=torch.empty(8, dtype=torch.uint8, device="cuda"))
     assert e.value.status == B.AQT_ERR_WORKSPACE
     with pytest.raises(TypeError):
+        B.aqt_attention_cached_fwd(rows, cache, 3, 2, ws=torch.empty(1 << 16, dtype=torch.uint8))
+    with pytest.raises(TypeError):
+        B.aqt_cache_append(rows, cache, 3, 2, dev_status=torch.zeros(1, dtype=torch.int32))
+    with pytest.raises(AttributeError):
+        cache.length = torch.zeros(2, dtype=torch.int64, device="cuda")
+    with pytest.raises(TypeError):
         B.KvCache(2, 64, 1, 8, length=torch.zeros(3, dtype=torch.int64, device="cuda"))
     with pytest.raises(B.AqtError):
         B.KvCache(2, 65, 1, 8)

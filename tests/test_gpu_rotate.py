@@ -246,3 +246,13 @@ def test_binding_refuses():
         B.QkNormRotate(2, 1, 8, rot=7)
     with pytest.raises(B.AqtError):
         B.aqt_qk_norm_rotate_fwd(x, 2, 3, B.QkNormRotate(2, 1, 8, pairing=3))
+    for ws in (torch.empty(1 << 24, dtype=torch.uint8), torch.empty(1 << 22, device="cuda")):
+        with pytest.raises(TypeError):
+            B.aqt_qk_norm_rotate_bwd(x, x.clone(), 2, 3, spec, ws=ws)
+    with pytest.raises(ValueError):
+        B.QkNormRotate(2, 1, 8, device="cpu")
+    spec.device = 1                                                  # gains and turns of another device's
+    with pytest.raises(ValueError):
+        B.aqt_qk_norm_rotate_fwd(x, 2, 3, spec)
+    with pytest.raises(ValueError):
+        B.aqt_qk_norm_rotate_bwd(x, x.clone(), 2, 3, spec)
