@@ -14,7 +14,7 @@
 namespace aqt {
 namespace {
 
-constexpr int kThreads = 256, kThreadsMax = 1024;
+constexpr int kThreads = 256;
 typedef float v4f __attribute__((ext_vector_type(4)));
 
 // Four dwords of four bytes each, transposed: out[i] byte f = in[f] byte i.
@@ -55,7 +55,8 @@ struct Quad {
 };
 // A stream's work, counted in items: runs of `run` quads (a power of two, aligned: 16 make a tile), the run's quads the fastest, then
 // keys or values and head, then runs.  So a workgroup writes the tiles it touches whole: frames of one head that eight
-// workgroups on eight L2s share cost every line eight partial writes (4096 frames of 16 streams: 140 us, 90 so; read back 118, 66).
+// workgroups on eight L2s share cost every line eight partial writes (4096 frames of 16 streams
+// with runs of one quad: written in 130 us, 69 so; read back in 93, 57).
 __device__ __forceinline__ Quad quad_of(const CacheGeom &g, int item, int log2_run, int64_t from) {
   const int per = 2 * g.kv_heads, group = item >> log2_run, r = group / per, w = group - r * per;
   const bool values = w >= g.kv_heads;
@@ -79,11 +80,13 @@ __device__ __forceinline__ uint8_t *tile_of(const CacheGeom &g, int64_t b, const
   return g.data + at * g.tile_bytes;
 }
 
+// A float32 row is not read again: without a place in the caches it leaves them to the codes and to what else is under way
+// (4096 frames of 16 streams, written and read back in turn: 92 and 64 us, 69 and 57 so).
 template <bool VEC>
 __device__ __forceinline__ void load4(float (&x)[4], const float *row, int col, int dh) {
   if (VEC) {
     if (col < dh) {
-      const v4f v = *reinterpret_cast<const v4f *>(row + col);
+      const v4f v = __builtin_nontemporal_load(reinterpret_cast<const v4f *>(row + col));
       x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
     } else {
       x[0] = x[1] = x[2] = x[3] = 0.0f;
@@ -105,14 +108,14 @@ __device__ __forceinline__ void store4(const float (&x)[4], float *row, int col,
 }
 
 template <int L, bool VEC>
-__global__ __launch_bounds__(kThreadsMax) void cache_append_kernel(const float *__restrict__ qkv, CacheGeom g, int64_t T, int heads,
+__global__ __launch_bounds__(kThreads) void cache_append_kernel(const float *__restrict__ qkv, CacheGeom g, int64_t T, int heads,
                                                                 const int32_t *__restrict__ count, int log2_run, int blocks_per_stream,
                                                                 int32_t *__restrict__ dev_status) {
   const int tid = static_cast<int>(threadIdx.x), j = tid % L;
   const int b = static_cast<int>(blockIdx.x) / blocks_per_stream, block = static_cast<int>(blockIdx.x) - b * blocks_per_stream;
   const StreamFrames f = stream_frames(g, count, T, b);
   const int64_t from = f.length > f.oldest ? f.length : f.oldest;   // later frames of this call take the place of those before
-  const Quad q = quad_of(g, block * (static_cast<int>(blockDim.x) / L) + tid / L, log2_run, from);
+  const Quad q = quad_of(g, block * (kThreads / L) + tid / L, log2_run, from);
   const int64_t ld = (static_cast<int64_t>(heads) + 2 * static_cast<int64_t>(g.kv_heads)) * g.dh;
   const int64_t at = (heads + (q.values ? g.kv_heads : 0) + static_cast<int64_t>(q.h)) * g.dh;
   const Columns<L> c(j, g.packed, q.values);
@@ -202,7 +205,7 @@ __device__ __forceinline__ void codes_of(float (&x)[4], uint32_t w, bool packed,
 }
 
 template <int L, bool VEC>
-__global__ __launch_bounds__(kThreadsMax) void cache_read_kernel(CacheGeom g, int64_t pending, const int32_t *__restrict__ count,
+__global__ __launch_bounds__(kThreads) void cache_read_kernel(CacheGeom g, int64_t pending, const int32_t *__restrict__ count,
                                                               const int64_t *__restrict__ first, int64_t n, int log2_run,
                                                               int blocks_per_stream, float *__restrict__ keys, float *__restrict__ values) {
   const int tid = static_cast<int>(threadIdx.x), j = tid % L;
@@ -211,7 +214,7 @@ __global__ __launch_bounds__(kThreadsMax) void cache_read_kernel(CacheGeom g, in
   const int64_t far = int64_t(1) << 61;
   int64_t from = first ? first[b] : f.end - n;
   from = from < -far ? -far : from > far ? far : from;
-  const Quad q = quad_of(g, block * (static_cast<int>(blockDim.x) / L) + tid / L, log2_run, from);
+  const Quad q = quad_of(g, block * (kThreads / L) + tid / L, log2_run, from);
   if (q.frame >= from + n || q.frame + 3 < from) return;
   float *const to = q.values ? values : keys;
   if (!to) return;
@@ -280,25 +283,23 @@ __global__ void cache_advance_kernel(int64_t *__restrict__ length, int64_t strea
 // How a call over `n` consecutive frames of every stream is cut up.
 struct Cut {
   int log2_run;
-  int threads;
   int64_t items, blocks;   // of a stream
 };
 int lanes_of(int dh) { return dh <= 32 ? 4 : dh <= 64 ? 8 : 16; }
 Cut cut_of(const CacheGeom &g, int64_t n) {
   const int64_t quads = (n + 2) / 4 + 1;   // that n frames can touch
-  Cut c{0, 0, 0, 0};
+  Cut c{0, 0, 0};
   while (c.log2_run < 4 && (int64_t(1) << c.log2_run) < quads) ++c.log2_run;
   const int64_t runs = ((quads - 2) >> c.log2_run) + 2;   // and as many runs of them, wherever the first begins
   c.items = ((quads == 1 ? 1 : runs) << c.log2_run) * 2 * g.kv_heads;
-  c.threads = c.items >= 8192 ? kThreadsMax : kThreads;
-  c.blocks = cdiv(c.items, c.threads / lanes_of(g.dh));
+  c.blocks = cdiv(c.items, kThreads / lanes_of(g.dh));
   return c;
 }
 // Items of a stream and workgroups of the launch count in 32 bits.
 bool grid_ok(const CacheGeom &g, int64_t n) {
   if (n > (int64_t(1) << 40)) return false;
   const Cut c = cut_of(g, n);
-  return c.items <= INT32_MAX - kThreadsMax && c.blocks <= INT32_MAX / g.streams;
+  return c.items <= INT32_MAX - kThreads && c.blocks <= INT32_MAX / g.streams;
 }
 
 }  // namespace
@@ -337,7 +338,7 @@ aqt_status launch_cache_append(const float *qkv, int64_t T, int heads, const aqt
   auto kern = c.dh <= 32   ? (vec ? cache_append_kernel<4, true> : cache_append_kernel<4, false>)
               : c.dh <= 64 ? (vec ? cache_append_kernel<8, true> : cache_append_kernel<8, false>)
                            : (vec ? cache_append_kernel<16, true> : cache_append_kernel<16, false>);
-  kern<<<static_cast<unsigned>(cut.blocks * c.streams), cut.threads, 0, st>>>(qkv, g, T, heads, count, cut.log2_run, static_cast<int>(cut.blocks),
+  kern<<<static_cast<unsigned>(cut.blocks * c.streams), kThreads, 0, st>>>(qkv, g, T, heads, count, cut.log2_run, static_cast<int>(cut.blocks),
                                                                           dev_status);
   AQT_HIP(hipGetLastError());
   return AQT_OK;
@@ -352,7 +353,7 @@ aqt_status launch_cache_read(const aqt_cache &c, int64_t pending, const int32_t 
   auto kern = c.dh <= 32   ? (vec ? cache_read_kernel<4, true> : cache_read_kernel<4, false>)
               : c.dh <= 64 ? (vec ? cache_read_kernel<8, true> : cache_read_kernel<8, false>)
                            : (vec ? cache_read_kernel<16, true> : cache_read_kernel<16, false>);
-  kern<<<static_cast<unsigned>(cut.blocks * c.streams), cut.threads, 0, st>>>(g, pending, count, first, n, cut.log2_run,
+  kern<<<static_cast<unsigned>(cut.blocks * c.streams), kThreads, 0, st>>>(g, pending, count, first, n, cut.log2_run,
                                                                           static_cast<int>(cut.blocks), keys, values);
   AQT_HIP(hipGetLastError());
   return AQT_OK;

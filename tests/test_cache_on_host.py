@@ -27,6 +27,7 @@ def spliced():
             "  const bool shift = ctrl < 0x120, on = (rows >> (l >> 4) & 1) && (shift ? (l & 15u) >= (unsigned)(ctrl & 15) : ctrl == 0x142 ? l >= 16u : l >= 32u);\n"
             "  const int from = lane_value(v, on ? (shift ? l - (unsigned)(ctrl & 15) : ctrl == 0x142 ? (l & 48u) - 1u : 31u) : l);\n"
             "  return on ? from : old;\n}\n"
+            "template <class V> inline V __builtin_nontemporal_load(const V *p) { return *p; }\n"
             "inline float __builtin_amdgcn_rsqf(float x) { return 1.0f / sqrtf(x); }\n"
             "inline float __shfl(float v, int lane) { return lane_value(v, (unsigned)lane); }\n")
     # a vector of two or four ints, by its length
