@@ -222,6 +222,7 @@ def _ptr(t: Optional[torch.Tensor]):
 
 # the current stream's handle; the public way to it builds a Stream object, a third of a short call's time on the host
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device   # where a tensor is on a device already
 
 
 def _stream():
@@ -893,7 +894,7 @@ def _shaped(t: Optional[torch.Tensor], dtype, shape: tuple, device: int, name: s
 def _current(t: torch.Tensor, name: str) -> int:
     """The index of the device that the tensor is on: the current one, whose current stream takes the launches."""
     device = t.get_device()
-    if device < 0 or device != torch.cuda.current_device():
+    if device < 0 or device != _device():
         raise ValueError(f"{name}: expected a tensor on the current device")
     return device
 
@@ -1026,15 +1027,18 @@ def aqt_cache_read(cache: KvCache, n: int, *, first=None, pending: int = 0, coun
     the last n).  pending / count: appended frames that cache.length does not count yet."""
     dev = _current(cache.data, "cache")
     shape = (cache.streams * n, cache.kv_heads * cache.dh)
-    _shaped(first, torch.int64, (cache.streams,), dev, "first")
-    _shaped(count, torch.int32, (cache.streams,), dev, "count")
+    if first is not None:
+        _shaped(first, torch.int64, (cache.streams,), dev, "first")
+    if count is not None:
+        _shaped(count, torch.int32, (cache.streams,), dev, "count")
     if want_keys:
         keys = torch.empty(shape, dtype=torch.float32, device=cache.data.device) if keys is None else _shaped(keys, torch.float32, shape, dev, "keys")
     if want_values:
         values = torch.empty(shape, dtype=torch.float32, device=cache.data.device) if values is None else _shaped(values, torch.float32, shape, dev, "values")
     keys, values = keys if want_keys else None, values if want_values else None
     _check(lib().aqt_cache_read(cache.ref, pending, None if count is None else count.data_ptr(),
-                                None if first is None else first.data_ptr(), n, _ptr(keys), _ptr(values), _raw_stream(dev)), "aqt_cache_read")
+                                None if first is None else first.data_ptr(), n, None if keys is None else keys.data_ptr(),
+                                None if values is None else values.data_ptr(), _raw_stream(dev)), "aqt_cache_read")
     return keys, values
 
 
