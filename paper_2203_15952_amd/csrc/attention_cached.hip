@@ -87,7 +87,7 @@ __global__ __launch_bounds__(kThreads, many_waves(DT, PACKED)) void attention_ca
   }
 
   // A tile's codes and scales are requested where the tile before has given up their registers: the keys' trip from memory passes
-  // under the rest of that tile, the values' under this one's scores (8 streams of 128 rows: 66 us with both at the head of a tile, 63 so).
+  // under the rest of that tile, the values' under this one's scores (8 streams of 128 rows: 60 us with both at the head of a tile, 57 so).
   typedef int key_piece __attribute__((ext_vector_type(KEYS)));
   key_piece keys[4][KS];
   v4i values[VALUES];
@@ -419,11 +419,11 @@ CachedCut cut_of(const CacheGeom &g, int64_t rows, int64_t window) {
   c.row_tiles = static_cast<int>(cdiv(rows, c.rows));
   c.groups = g.streams * g.kv_heads * c.row_tiles;
   // As many workgroups as the chip holds at a time, a wavefront of each on every SIMD: what comes behind them would form its rows' digits
-  // and request its first tile while the others work (32 streams, four rows of 128 columns: 108 us with 512 workgroups, 113 with
-  // 1024, 123 with 2048; 8 streams of 128 rows: 64 us with 512, 67 with 1024, 74 with 2048).
+  // and request its first tile while the others work (32 streams, four rows of 128 columns: 109 us with 512 or 1024
+  // workgroups, 116 with 2048; 8 streams of 128 rows: 57 us with 512, 62 with 1024, 76 with 2048).
   const int64_t want = 256 * (c.rows <= kFewRows ? few_waves(dt, g.packed, c.rows) : many_waves(dt, g.packed)) / c.groups;
   // A split has its price, the second launch: under kSplitTiles it takes longer than the tiles that it saves (32 streams of 16 frames with a
-  // window of 5 tiles: 11.1 us in two splits, 8.8 in one), and a wavefront gets two tiles at least.
+  // window of 5 tiles: 11.0 us in two splits, 9.0 in one), and a wavefront gets two tiles at least.
   const int64_t tiles = cdiv(window, 64) + 1, most = tiles < kSplitTiles ? 1 : tiles / (2 * kWaves), s = want < most ? want : most;
   c.splits = static_cast<int>(s < 1 ? 1 : s);
   return c;

@@ -1,8 +1,8 @@
 // Attention over the quantized cache where at most four rows (new frame, query head) share a key / value head: single frames, with
 // or without grouped heads.  The digits and products of attention_cached.hip; there a lane holds sixteen scores of one of
 // sixteen rows, which for one row is sixteen times the vector work that there is (16 streams, one frame over 4000 to 16000 frames,
-// int8: 41 us, 31 here; 32 streams, four rows, heads of 128, int4: 169 us, 109 here; reading the codes takes 23 and 88).  Here a lane holds one frame's score for
-// each row, and one column of the result:
+// int8: 32 us, 27 here; 32 streams, four rows, heads of 128, int4: 109 us, 104 here; reading the codes takes 23 and 88).  Here a lane
+// holds one frame's score for each row, and one column of the result:
 //   S (rows x 64 frames) = q K^T   A operand: the rows, repeated in each group of four; B operand: 16 frames at a time.  All four groups
 //                                  of lanes then hold the scores of all 16; group g keeps those of the g-th 16
 //   O (rows x dh) = P V            A operand: the probabilities' digits, through LDS (a byte per digit); B operand: value rows.  Again
@@ -80,7 +80,7 @@ __global__ __launch_bounds__(kThreads, few_waves(DT, PACKED, R)) void attention_
   uint8_t *const put = &digits[wave][0][0][frame_slot(lane)];
   const uint8_t *const take = &digits[wave][0][min(lr & 3, R - 1)][16 * lg];
   // A tile's keys, values and scales are requested where the tile before has given up their registers: the keys' trip from memory
-  // passes under the rest of that tile, the values' under this one's scores (32 streams, four rows, int4: 132 us with all loads at the head of a tile, 118 so).
+  // passes under the rest of that tile, the values' under this one's scores.
   constexpr int KEYS = PACKED ? 2 : 4, VALUES = PACKED ? DT / 2 : DT;
   typedef int key_piece __attribute__((ext_vector_type(KEYS)));
   key_piece keys[4][KS];
