@@ -294,6 +294,27 @@ def test_a_cache_beyond_4_gib(T, group):
     np.testing.assert_array_equal(host(values).reshape(50, kv, dh), ref.frames("v", 0, first, 50))
 
 
+def test_rows_beyond_2_to_31_elements():
+    """A million frames at once: the last ones come out of the cache, and attend, as they do in a small call.  The outputs of the two
+    calls are each within tolerance() of the same value; with scores under 16 and at most 4 frames that is (226 + 134) U of max|v|."""
+    T, heads, kv, dh = 1 << 20, 16, 16, 128
+    say("large rows", T)
+    rows = torch.randn((T, (heads + 2 * kv) * dh), device="cuda", generator=torch.Generator(device="cuda").manual_seed(0))
+    cache, small = B.KvCache(1, T, kv, dh), B.KvCache(1, 256, kv, dh)
+    B.aqt_cache_append(rows, cache, T, heads)
+    B.aqt_cache_append(rows[-200:-100], small, 100, heads)
+    small.advance(100)
+    B.aqt_cache_append(rows[-100:], small, 100, heads)
+    for big, want in zip(B.aqt_cache_read(cache, T, pending=T), B.aqt_cache_read(small, 200, pending=100)):
+        assert big.numel() >= 1 << 31 and torch.equal(big[-200:], want)
+        del big
+    ctx, _ = B.aqt_attention_cached_fwd(rows, cache, T, heads, left=3)
+    assert ctx.numel() >= 1 << 31
+    want, _ = B.aqt_attention_cached_fwd(rows[-100:], small, 100, heads, left=3)
+    top = float(rows[-200:, (heads + kv) * dh:].abs().max())
+    np.testing.assert_allclose(host(ctx[-100:]), host(want), rtol=0, atol=2 * 360 * U * top)
+
+
 def test_rows_that_see_nothing_are_zeros():
     """More new frames than the cache holds: the first ones' windows lie before its oldest frame."""
     cache, ref = make(1, 64, 2, 1, 32, 8)

@@ -205,6 +205,23 @@ def test_unaligned_tensors_and_given_turns():
     np.testing.assert_allclose(host(spec.turns), 10000.0 ** (-np.arange(8) / 8) / (2 * np.pi), rtol=1e-14)
 
 
+def test_more_than_2_to_30_rows():
+    """Rows and bytes that do not count in 32 bits: the last utterance and one in the middle come out as they do by themselves."""
+    B_, T, spec = 1025, 1 << 20, B.QkNormRotate(1, 1, 2)
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    say("many rows", B_, T)
+    x = torch.randn((B_ * T, 6), device="cuda", generator=gen)
+    dy = torch.randn((B_ * T, 6), device="cuda", generator=gen)
+    first = torch.arange(B_, dtype=torch.int64, device="cuda") * 1000
+    some = [(b, slice(b * T, (b + 1) * T)) for b in (513, B_ - 1)]
+    alone = [(B.aqt_qk_norm_rotate_fwd(x[at], 1, T, spec, first=first[b:b + 1]),
+              B.aqt_qk_norm_rotate_bwd(x[at], dy[at], 1, T, spec, first=first[b:b + 1], want_gamma=False)[0]) for b, at in some]
+    B.aqt_qk_norm_rotate_bwd(x, dy, B_, T, spec, first=first, dqkv=dy, want_gamma=False)
+    B.aqt_qk_norm_rotate_fwd(x, B_, T, spec, first=first, out=x)
+    for (b, at), (y, dx) in zip(some, alone):
+        assert torch.equal(x[at], y) and torch.equal(dy[at], dx)
+
+
 def test_special_values_stay_in_their_head():
     """A NaN, an infinity and a head of zeros: what the formula gives there, and nothing in the heads beside them."""
     heads, kv, dh = 4, 4, 64
