@@ -9,6 +9,7 @@
 // value row, whose four frames are neighbours, as dwords of four frames after a 4 x 4 transposition of bytes in registers.  Where a
 // call brings only some of the four frames the others' bytes are not touched.
 #include "cache.h"
+#include "lanes.h"
 #include "quant_code.h"
 
 namespace aqt {
@@ -27,9 +28,9 @@ __device__ __forceinline__ void transpose_bytes(uint32_t (&w)[4]) {
   w[3] = __builtin_amdgcn_perm(cd1, ab1, 0x07060302u);
 }
 
-// Four codes, the first in the lowest byte.  r is 1 / s to 2^-23 of it: then x r is within 2^-14 of x / s, and where it lies no nearer than 2^-13
-// to the middle between two whole numbers its nearest one is the floor that defines the code; otherwise (one quad in a thousand)
-// the four are divided.  x r + 1.5 2^23 rounds to that whole number, in its lowest bits.  No value exceeds its group's maximum, so no
+// Four codes, the first in the lowest byte.  r is 1 / s to 2^-23 of it: then x r is within 2^-16 of x / s (up to 127), whose own rounding
+// and that of the sum with 1 / 2 are 2^-18 each, and where it lies no nearer than 2^-14 to the middle between two whole numbers its
+// nearest one is the floor that defines the code; otherwise (one quad in two thousand) the four are divided.  x r + 1.5 2^23 rounds to that whole number, in its lowest bits.  No value exceeds its group's maximum, so no
 // code is clamped.  r is 0 where s is no ordinary number.
 __device__ __forceinline__ uint32_t codes4(const float (&x)[4], float s, float r, float fq) {
   constexpr float kWhole = 12582912.0f;
@@ -41,7 +42,7 @@ __device__ __forceinline__ uint32_t codes4(const float (&x)[4], float s, float r
     n[e] = __float_as_uint(w);
     off[e] = fabsf(fmaf(x[e], r, kWhole - w));
   }
-  if (r == 0.0f || !(fmaxf(fmaxf(off[0], off[1]), fmaxf(off[2], off[3])) < 0.5f - 0x1p-13f))
+  if (r == 0.0f || !(fmaxf(fmaxf(off[0], off[1]), fmaxf(off[2], off[3])) < 0.5f - 0x1p-14f))
     return quant4_divided(x[0], x[1], x[2], x[3], Quantizer{s, fq, 0.0f, false});
   const uint32_t lo = __builtin_amdgcn_perm(n[1], n[0], 0x0C0C0400u), hi = __builtin_amdgcn_perm(n[3], n[2], 0x0C0C0400u);
   return __builtin_amdgcn_perm(hi, lo, 0x05040100u);
@@ -132,26 +133,36 @@ __global__ __launch_bounds__(kThreads) void cache_append_kernel(const float *__r
   }
   uint8_t *const tile = tile_of(g, b, q);
   const int key = static_cast<int>(q.frame & 63);
-  uint32_t code[2][4];   // [half][frame]
+  // A lane divides for one of the four frames and hands on.
+  uint32_t top[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    code[0][i] = code[1][i] = 0u;
+    top[i] = 0u;
     if (!__any(mine[i])) continue;   // single frames: three of the four
     uint32_t m = 0u;
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int e = 0; e < 4; ++e) m = max(m, __float_as_uint(x[i][h][e]) & 0x7FFFFFFFu);
+    top[i] = group_max<L>(m);
+  }
+  const bool odd = j & 1, upper = j & 2, own = upper ? (odd ? mine[3] : mine[2]) : odd ? mine[1] : mine[0];
+  const uint32_t own_top = upper ? (odd ? top[3] : top[2]) : odd ? top[1] : top[0];
+  const float fq = static_cast<float>(g.qmax), own_s = __uint_as_float(own_top) / fq;
+  const float own_r = own_s > 0x1p-60f && own_s < 0x1p60f ? __builtin_amdgcn_rcpf(own_s) : 0.0f;
+  if (j < 4 && own) {
+    reinterpret_cast<float *>(tile + cache_scales(g))[(q.values ? 64 : 0) + key + j] = own_s;
+    if (dev_status && own_top >= 0x7F800000u) *dev_status = AQT_ERR_NONFINITE;
+  }
+  const float s[4] = {of_four<0>(own_s), of_four<1>(own_s), of_four<2>(own_s), of_four<3>(own_s)};
+  const float r[4] = {of_four<0>(own_r), of_four<1>(own_r), of_four<2>(own_r), of_four<3>(own_r)};
+  uint32_t code[2][4];   // [half][frame]
 #pragma unroll
-    for (int off = 1; off < L; off <<= 1) m = max(m, static_cast<uint32_t>(__shfl_xor(static_cast<int>(m), off, 64)));
-    const float fq = static_cast<float>(g.qmax), s = __uint_as_float(m) / fq;
-    const float r = s > 0x1p-60f && s < 0x1p60f ? __builtin_amdgcn_rcpf(s) : 0.0f;
+  for (int i = 0; i < 4; ++i) {
+    code[0][i] = code[1][i] = 0u;
+    if (!__any(mine[i])) continue;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) code[h][i] = codes4(x[i][h], s, r, fq);
-    if (j == 0 && mine[i]) {
-      reinterpret_cast<float *>(tile + cache_scales(g))[(q.values ? 64 : 0) + key + i] = s;
-      if (dev_status && m >= 0x7F800000u) *dev_status = AQT_ERR_NONFINITE;
-    }
+    for (int h = 0; h < 2; ++h) code[h][i] = codes4(x[i][h], s[i], r[i], fq);
   }
   if (!q.values) {
 #pragma unroll

@@ -7,15 +7,15 @@
 // The normaliser is formed again from x (it is in registers), so the forward keeps nothing.
 //
 // Memory bounds both directions: a row is read once and written once.  A group of LANES lanes owns one head at a time and a
-// lane the same columns of every head, so gamma, its gradient and the cosines stay in registers while the group walks the
-// heads of its row; a wavefront walks a run of rows.  A lane's columns are whole pairs, so rotating takes no exchange: for
+// lane the same columns of every head, so the gains' gradients and the cosines stay in registers while the group walks the
+// heads of its row; the wavefronts walk the rows side by side.  A lane's columns are whole pairs, so rotating takes no exchange: for
 // halves (i, i + rot / 2) the 16-byte pieces at j and rot / 8 + j, for neighbours (2 i, 2 i + 1) two adjacent pieces.  Heads
 // that are not whole pieces, or not aligned, take single columns and shuffles for the partner (`Single`).
 //
 // The angle is exact where it matters: frame * turns in float64, reduced there to an eighth of a turn around the nearest
 // quarter, and only that remainder goes on in float32 (a position of a million frames costs no accuracy; in float32 its
 // angle would be off by 0.06).
-#include "aqt_internal.h"
+#include "lanes.h"
 
 namespace aqt {
 namespace {
@@ -162,13 +162,6 @@ struct Single {
     x[1] = y[1];
   }
 };
-
-template <int L>
-__device__ __forceinline__ float group_sum(float v) {
-#pragma unroll
-  for (int off = 1; off < L; off <<= 1) v += __shfl_xor(v, off, 64);
-  return v;
-}
 
 // BWD: y is the upstream gradient, out the gradient with respect to x, part (nullable) [workgroups][2][dh] column sums.
 template <class F, bool BWD>

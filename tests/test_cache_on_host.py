@@ -24,6 +24,9 @@ def spliced():
             # the data-parallel primitives of a maximum over the wavefront: row_shr:n, row_bcast:15, row_bcast:31
             "inline int __builtin_amdgcn_update_dpp(int old, int v, int ctrl, int rows, int, bool) {\n"
             "  const unsigned l = threadIdx.x & 63u;\n"
+            # moves that every lane takes part in: a permutation of four, mirror images in 16 and in 8
+            "  if (ctrl < 0x100) return lane_value(v, (l & ~3u) | ((unsigned)ctrl >> 2 * (l & 3u) & 3u));\n"
+            "  if (ctrl == 0x140 || ctrl == 0x141) return lane_value(v, l ^ (ctrl == 0x140 ? 15u : 7u));\n"
             "  const bool shift = ctrl < 0x120, on = (rows >> (l >> 4) & 1) && (shift ? (l & 15u) >= (unsigned)(ctrl & 15) : ctrl == 0x142 ? l >= 16u : l >= 32u);\n"
             "  const int from = lane_value(v, on ? (shift ? l - (unsigned)(ctrl & 15) : ctrl == 0x142 ? (l & 48u) - 1u : 31u) : l);\n"
             "  return on ? from : old;\n}\n"
@@ -32,7 +35,7 @@ def spliced():
             "inline float __shfl(float v, int lane) { return lane_value(v, (unsigned)lane); }\n")
     # a vector of two or four ints, by its length
     shim += "template <int N> struct key_piece_of { typedef v4i type; };\ntemplate <> struct key_piece_of<2> { typedef v2i type; };\n"
-    return (shim + helpers + layout + read("quant_code.h") + kernels("cache.hip", "cache_", "}  // namespace\n\nbool cache_shape_ok") +
+    return (shim + helpers + layout + read("lanes.h").replace('#include "aqt_internal.h"', "") + read("quant_code.h") + kernels("cache.hip", "cache_", "}  // namespace\n\nbool cache_shape_ok") +
             shared + kernels("attention_cached_few.hip", "few", "template <int DT, bool PACKED>\naqt_status launch_rows").replace(
                 "typedef int key_piece __attribute__((ext_vector_type(KEYS)));", "typedef typename key_piece_of<KEYS>::type key_piece;") +
             kernels("attention_cached.hip", "attend", "constexpr int64_t kSplitTiles").replace(
