@@ -448,7 +448,7 @@ void launch_join(const float *part, const CacheGeom &g, const CachedGeom &a, con
 bool cached_attention_ok(const aqt_cache &c, int64_t T, int heads) {
   if (T > (int64_t(1) << 24)) return false;
   const int64_t rows = T * (heads / c.kv_heads), row_tiles = cdiv(rows, rows <= kFewRows ? rows : kRows);
-  return row_tiles * kRows <= (int64_t(1) << 30) && row_tiles * c.kv_heads <= (int64_t(1) << 30) / c.streams;
+  return row_tiles * kRows <= (int64_t(1) << 30) && row_tiles * c.kv_heads <= kMostBlocks / c.streams;
 }
 
 size_t cached_attention_ws_bytes(const aqt_cache &c, int64_t T, int heads) {

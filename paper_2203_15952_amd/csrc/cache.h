@@ -51,6 +51,8 @@ __host__ __device__ inline StreamFrames stream_frames(const CacheGeom &g, const 
   return StreamFrames{L, end, end > cap ? end - cap : 0};
 }
 
+constexpr int64_t kMostBlocks = (int64_t(1) << 24) - 1;   // of 256 threads: a launch's threads count in 32 bits
+
 bool cache_shape_ok(const aqt_cache &c);
 CacheGeom cache_geom(const aqt_cache &c);
 aqt_status launch_cache_append(const float *qkv, int64_t T, int heads, const aqt_cache &c, const int32_t *count, hipStream_t st,

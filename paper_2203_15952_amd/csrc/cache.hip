@@ -306,11 +306,11 @@ Cut cut_of(const CacheGeom &g, int64_t n) {
   c.blocks = cdiv(c.items, kThreads / lanes_of(g.dh));
   return c;
 }
-// Items of a stream and workgroups of the launch count in 32 bits.
+// Items of a stream count in 32 bits, and so do the threads of the launch.
 bool grid_ok(const CacheGeom &g, int64_t n) {
   if (n > (int64_t(1) << 40)) return false;
   const Cut c = cut_of(g, n);
-  return c.items <= INT32_MAX - kThreads && c.blocks <= INT32_MAX / g.streams;
+  return c.items <= INT32_MAX - kThreads && c.blocks <= kMostBlocks / g.streams;
 }
 
 }  // namespace

@@ -105,6 +105,12 @@ def test_cache_calls_refuse_arguments(L):
     assert att(ONE, 1, 4, c, None, -1, 0, BIG, None, None, need, None) == WORKSPACE
     assert att(ONE, 1, 4, c, None, -1, 0, BIG, None, ONE, need - 1, None) == WORKSPACE
     assert att(ONE, 1 << 25, 4, c, None, -1, 0, BIG, None, ONE, BIG, None) == UNSUPPORTED
+    many = cache(streams=1 << 24, kv_heads=1)                                               # 2^32 threads and more in a launch
+    assert app(ONE, 1, 1, many, None, None, None) == UNSUPPORTED
+    assert L.aqt_cache_read(many, 0, None, None, 1, ONE, ONE, None) == UNSUPPORTED
+    assert L.aqt_attention_cached_workspace_bytes(many, 1, 1) == 0
+    assert att(ONE, 1, 1, many, None, -1, 0, BIG, None, ONE, BIG, None) == UNSUPPORTED
+    assert att(ONE, 1 << 14, 16, cache(streams=1 << 10, kv_heads=16, dh=8), None, -1, 0, BIG, None, ONE, BIG, None) == UNSUPPORTED
     adv = L.aqt_cache_advance
     assert adv(None, 2, 1, None, None) == INVALID and adv(ONE, 0, 1, None, None) == INVALID and adv(ONE, 2, 0, None, None) == INVALID
 
