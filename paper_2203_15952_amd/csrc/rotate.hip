@@ -10,7 +10,7 @@
 // lane the same columns of every head, so the gains' gradients and the cosines stay in registers while the group walks the
 // heads of its row; the wavefronts walk the rows side by side.  A lane's columns are whole pairs, so rotating takes no exchange: for
 // halves (i, i + rot / 2) the 16-byte pieces at j and rot / 8 + j, for neighbours (2 i, 2 i + 1) two adjacent pieces.  Heads
-// that are not whole pieces, or not aligned, take single columns and shuffles for the partner (`Single`).
+// that are not whole pieces, or not aligned, or whose rotated halves are not, meet their pairs' other halves in LDS (`Apart`).
 //
 // The angle is exact where it matters: frame * turns in float64, reduced there to an eighth of a turn around the nearest
 // quarter, and only that remainder goes on in float32 (a position of a million frames costs no accuracy; in float32 its
@@ -68,7 +68,7 @@ __device__ __forceinline__ Angle angle_of(double turn) {
 // Eight columns of a head in two 16-byte pieces: lane j of the group.
 template <int L, bool HALVES>
 struct Pieces {
-  static constexpr int LANES = L, N = 8, ANGLES = 4, PAIRS = 4 * L;   // PAIRS: of a head, at most
+  static constexpr int LANES = L, N = 8, ANGLES = 4, PAIRS = 4 * L, SCRATCH = 4;   // PAIRS: of a head, at most
   int at[2];       // the pieces' first columns
   bool has[2];
   int pair;        // the first of this lane's four pairs
@@ -110,7 +110,7 @@ struct Pieces {
     for (int h = 0; h < 2; ++h)
       if (has[h]) *reinterpret_cast<v4f *>(p + at[h]) = v4f{x[4 * h], x[4 * h + 1], x[4 * h + 2], x[4 * h + 3]};
   }
-  __device__ __forceinline__ void turn(float (&x)[N], const Angle (&t)[ANGLES], bool back) const {
+  __device__ __forceinline__ void turn(float (&x)[N], const Angle (&t)[ANGLES], bool back, float *) const {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const int ia = HALVES ? i : 2 * i, ib = HALVES ? i + 4 : 2 * i + 1;
@@ -121,45 +121,74 @@ struct Pieces {
   }
 };
 
-// Two columns of a head, j and j + L: any head width and alignment.
-template <int L, bool HALVES>
-struct Single {
-  static constexpr int LANES = L, N = 2, ANGLES = 2, PAIRS = L;
+// Eight columns of a head whose pairs another lane may hold the other half of: any width, alignment and number of rotated columns.
+// VEC: two 16-byte pieces, on 16-byte boundaries, where only the rotated halves are no whole pieces; otherwise every L-th column,
+// so that the lanes of a load are neighbours.
+template <int L, bool HALVES, bool VEC>
+struct Apart {
+  static_assert(HALVES || !VEC, "neighbours on 16-byte boundaries: Pieces");
+  static constexpr int LANES = L, N = 8, ANGLES = 8, PAIRS = 4 * L, SCRATCH = HALVES ? 512 : 4;
   int j, dh, rot;
-  __device__ __forceinline__ Single(int j_, int dh_, int rot_) : j(j_), dh(dh_), rot(rot_) {}
-  __device__ __forceinline__ int column(int i) const { return j + L * i; }
+  __device__ __forceinline__ Apart(int j_, int dh_, int rot_) : j(j_), dh(dh_), rot(rot_) {}
+  __device__ __forceinline__ int column(int i) const { return VEC ? 4 * j + (i & 3) + (i >> 2) * 4 * L : j + L * i; }
   __device__ __forceinline__ bool own(int i) const { return column(i) < dh; }
   __device__ __forceinline__ int pair_of(int i) const {
     const int c = column(i);
     return c >= rot ? 0 : HALVES ? (c < (rot >> 1) ? c : c - (rot >> 1)) : c >> 1;
   }
   __device__ __forceinline__ void load(float (&x)[N], const float *p, bool on) const {
+    if constexpr (VEC) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) x[i] = on && own(i) ? p[column(i)] : 0.0f;
+      for (int h = 0; h < 2; ++h) {
+        v4f v = {0.0f, 0.0f, 0.0f, 0.0f};
+        if (on && own(4 * h)) v = *reinterpret_cast<const v4f *>(p + column(4 * h));
+        x[4 * h] = v.x; x[4 * h + 1] = v.y; x[4 * h + 2] = v.z; x[4 * h + 3] = v.w;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) x[i] = on && own(i) ? p[column(i)] : 0.0f;
+    }
   }
-  __device__ __forceinline__ void load_gains(float (&x)[N], const float *p) const {
+  __device__ __forceinline__ void load_gains(float (&x)[N], const float *p) const {   // 128 of them, whatever the head
 #pragma unroll
-    for (int i = 0; i < 2; ++i) x[i] = p[own(i) ? column(i) : 0];
+    for (int i = 0; i < N; ++i) x[i] = p[column(i)];
   }
   __device__ __forceinline__ void store(const float (&x)[N], float *p) const {
+    if constexpr (VEC) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
-      if (own(i)) p[column(i)] = x[i];
+      for (int h = 0; h < 2; ++h)
+        if (own(4 * h)) *reinterpret_cast<v4f *>(p + column(4 * h)) = v4f{x[4 * h], x[4 * h + 1], x[4 * h + 2], x[4 * h + 3]};
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (own(i)) p[column(i)] = x[i];
+    }
   }
-  __device__ __forceinline__ void turn(float (&x)[N], const Angle (&t)[ANGLES], bool back) const {
-    const int base = static_cast<int>(threadIdx.x & 63u) - j, half = rot >> 1;
-    float y[2];
+  // head: the group's 8 L words of LDS, through which the halves meet
+  __device__ __forceinline__ void turn(float (&x)[N], const Angle (&t)[ANGLES], bool back, float *head) const {
+    const int half = rot >> 1;
+    float y[N];
+    if constexpr (HALVES) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+      for (int i = 0; i < N; ++i) head[column(i)] = x[i];
+      wave_lds_order();
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int c = column(i);
+        y[i] = head[c >= rot ? c : c < half ? c + half : c - half];
+      }
+      wave_lds_order();   // read before the next head's are written
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) y[i] = of_neighbour(x[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
       const int c = column(i);
       const bool second = HALVES ? c >= half : c & 1;
-      const int p = c >= rot ? c : HALVES ? (second ? c - half : c + half) : c ^ 1;   // the partner's column
-      const float lo = __shfl(x[0], base + (p & (L - 1))), hi = __shfl(x[1], base + (p & (L - 1)));
-      const float other = p < L ? lo : hi, s = back ? -t[i].s : t[i].s;
-      y[i] = c >= rot ? x[i] : second ? other * s + x[i] * t[i].c : x[i] * t[i].c - other * s;
+      const float s = second == back ? -t[i].s : t[i].s;
+      x[i] = c >= rot ? x[i] : x[i] * t[i].c + y[i] * s;
     }
-    x[0] = y[0];
-    x[1] = y[1];
   }
 };
 
@@ -177,6 +206,7 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const float *x, const 
   __shared__ __attribute__((aligned(16))) float gains[2][128];
   __shared__ double turns[kMaxPairs];
   __shared__ Angle angles[kThreads / 64][64 * 4];
+  __shared__ __attribute__((aligned(16))) float heads[kThreads / 64][F::SCRATCH];
   if (tid < 2 * 128) {
     const int w = tid >> 7, c = tid & 127;
     gains[w][c] = g.gamma[w] && c < g.dh ? g.gamma[w][c] : 1.0f;
@@ -184,6 +214,7 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const float *x, const 
   if (tid < kMaxPairs) turns[tid] = tid < g.rot / 2 ? g.turns[tid] : 0.0;
   const int row_lanes = L * g.per_row, place = sub * L + j;
   Angle *const row_angles = angles[tid >> 6] + row_of * PAIRS;
+  float *const head = F::SCRATCH > 4 ? heads[tid >> 6] + group * 8 * L : nullptr;
   float dgain[2][N];   // only where it is asked for (BWD)
 #pragma unroll
   for (int w = 0; w < 2; ++w)
@@ -253,13 +284,13 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const float *x, const 
 #pragma unroll
             for (int i = 0; i < N; ++i) u[i] = v[k][i];
           }
-          f.turn(u, a, false);
+          f.turn(u, a, false, head);
 #pragma unroll
           for (int i = 0; i < N; ++i) u[i] = value ? v[k][i] : u[i];
         } else {
 #pragma unroll
           for (int i = 0; i < N; ++i) u[i] = w[k][i];
-          f.turn(u, a, true);
+          f.turn(u, a, true, head);
           if (g.norm) {
             float gain[N], ss = 0.0f;
             f.load_gains(gain, gains[query ? 0 : 1]);
@@ -371,14 +402,24 @@ aqt_status launch_as(const float *x, const float *y, RotateGeom g, float *out, f
 template <bool HALVES, bool BWD>
 aqt_status launch_paired(const float *x, const float *y, const RotateGeom &g, float *out, float *part, bool aligned, hipStream_t st,
                          unsigned *blocks) {
-  // whole 16-byte pieces; in halves the rotated columns are whole pieces in either half too
-  if (aligned && g.dh % 4 == 0 && (!HALVES || g.rot % 8 == 0)) {
+  // Whole 16-byte pieces; in halves a lane has both of a pair only where either half is whole pieces too (25628 rows of 1536, heads of 64
+  // with 24 rotated columns: 61 us; with 18, whose pairs meet in LDS, 62, and 112 with single columns).
+  const bool pieces = aligned && g.dh % 4 == 0;
+  if (pieces && (!HALVES || g.rot % 8 == 0)) {
     if (g.dh <= 32) return launch_as<Pieces<4, HALVES>, BWD>(x, y, g, out, part, st, blocks);
     if (g.dh <= 64) return launch_as<Pieces<8, HALVES>, BWD>(x, y, g, out, part, st, blocks);
     return launch_as<Pieces<16, HALVES>, BWD>(x, y, g, out, part, st, blocks);
   }
-  if (g.dh <= 32) return launch_as<Single<16, HALVES>, BWD>(x, y, g, out, part, st, blocks);
-  return launch_as<Single<64, HALVES>, BWD>(x, y, g, out, part, st, blocks);
+  if constexpr (HALVES) {
+    if (pieces) {
+      if (g.dh <= 32) return launch_as<Apart<4, true, true>, BWD>(x, y, g, out, part, st, blocks);
+      if (g.dh <= 64) return launch_as<Apart<8, true, true>, BWD>(x, y, g, out, part, st, blocks);
+      return launch_as<Apart<16, true, true>, BWD>(x, y, g, out, part, st, blocks);
+    }
+  }
+  if (g.dh <= 32) return launch_as<Apart<4, HALVES, false>, BWD>(x, y, g, out, part, st, blocks);
+  if (g.dh <= 64) return launch_as<Apart<8, HALVES, false>, BWD>(x, y, g, out, part, st, blocks);
+  return launch_as<Apart<16, HALVES, false>, BWD>(x, y, g, out, part, st, blocks);
 }
 
 RotateGeom rotate_geom(int64_t B, int64_t T, const aqt_qk_norm_rotate &s, const int64_t *first, bool in_place) {

@@ -177,9 +177,13 @@ template <class F, bool BWD> static void turn_kernel(const float *x, const float
   g.stride_t = g.stride % g.T;
   run((unsigned)blocks, 256, 0, [&] { turn::rotate_kernel<F, BWD>(x, y, g, out, part); });
 }
-template <bool HALVES, bool BWD> static void turn_paired(const float *x, const float *y, const turn::RotateGeom &g, float *out, float *part, bool pieces, int blocks) {
-  if (pieces) { if (g.dh <= 32) turn_kernel<turn::Pieces<4, HALVES>, BWD>(x, y, g, out, part, blocks); else if (g.dh <= 64) turn_kernel<turn::Pieces<8, HALVES>, BWD>(x, y, g, out, part, blocks); else turn_kernel<turn::Pieces<16, HALVES>, BWD>(x, y, g, out, part, blocks); }
-  else { if (g.dh <= 32) turn_kernel<turn::Single<16, HALVES>, BWD>(x, y, g, out, part, blocks); else turn_kernel<turn::Single<64, HALVES>, BWD>(x, y, g, out, part, blocks); }
+// form 2: whole pieces with both of every pair; 1: whole pieces; 0: single columns
+template <bool HALVES, bool BWD> static void turn_paired(const float *x, const float *y, const turn::RotateGeom &g, float *out, float *part, int form, int blocks) {
+  if (form == 2) { if (g.dh <= 32) turn_kernel<turn::Pieces<4, HALVES>, BWD>(x, y, g, out, part, blocks); else if (g.dh <= 64) turn_kernel<turn::Pieces<8, HALVES>, BWD>(x, y, g, out, part, blocks); else turn_kernel<turn::Pieces<16, HALVES>, BWD>(x, y, g, out, part, blocks); }
+  else if (form == 1) {
+    if constexpr (HALVES) { if (g.dh <= 32) turn_kernel<turn::Apart<4, true, true>, BWD>(x, y, g, out, part, blocks); else if (g.dh <= 64) turn_kernel<turn::Apart<8, true, true>, BWD>(x, y, g, out, part, blocks); else turn_kernel<turn::Apart<16, true, true>, BWD>(x, y, g, out, part, blocks); }
+  }
+  else { if (g.dh <= 32) turn_kernel<turn::Apart<4, HALVES, false>, BWD>(x, y, g, out, part, blocks); else if (g.dh <= 64) turn_kernel<turn::Apart<8, HALVES, false>, BWD>(x, y, g, out, part, blocks); else turn_kernel<turn::Apart<16, HALVES, false>, BWD>(x, y, g, out, part, blocks); }
 }
 static void rotate_case(int64_t B, int64_t T, int heads, int kv, int dh, int rot, bool halves, bool norm, bool gains, bool first, bool in_place) {
   printf("rotate B %ld T %ld heads %d / %d dh %d rot %d halves %d norm %d gains %d\n", (long)B, (long)T, heads, kv, dh, rot, halves, norm, gains); fflush(stdout);
@@ -196,9 +200,9 @@ static void rotate_case(int64_t B, int64_t T, int heads, int kv, int dh, int rot
   turn::RotateGeom g{};
   g.T = T; g.M = B * T; g.ld = cols; g.heads = heads; g.kv_heads = kv; g.dh = dh; g.rot = rot; g.norm = norm; g.in_place = 0; g.eps = 1e-6f;
   g.turns = np ? turns : nullptr; g.first = first ? f0 : nullptr; g.gamma[0] = gains ? gq : nullptr; g.gamma[1] = gains ? gk : nullptr;
-  const bool can = dh % 4 == 0 && (!halves || rot % 8 == 0);
-  for (int pieces = can; pieces >= 0; --pieces) for (int blocks : {1, 3}) {
-    if (blocks == 1 && dh != 36) continue;
+  const int most = dh % 4 ? 0 : !halves || rot % 8 == 0 ? 2 : 1;
+  for (int pieces = most; pieces >= 0; --pieces) for (int blocks : {1, 3}) {
+    if ((blocks == 1 && dh != 36) || (pieces == 1 && !halves)) continue;
     float *part = floats((size_t)blocks * 2 * dh);
     if (halves) { turn_paired<true, false>(x, nullptr, g, out, nullptr, pieces, blocks); turn_paired<true, true>(norm ? x : nullptr, dy, g, dx, part, pieces, blocks); }
     else { turn_paired<false, false>(x, nullptr, g, out, nullptr, pieces, blocks); turn_paired<false, true>(norm ? x : nullptr, dy, g, dx, part, pieces, blocks); }
