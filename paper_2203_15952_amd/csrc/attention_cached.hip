@@ -9,7 +9,8 @@
 //
 // A workgroup owns 16 rows (frame, query head) that share a key / value head, and its wavefronts take the tiles of 64 frames
 // in turn, each with its own running maximum and sum, joined through LDS at the end; where that leaves the chip empty, several
-// workgroups (splits) share the tiles and a second launch joins what they leave behind.  Both products are formed transposed,
+// workgroups (splits) share the tiles and a second launch joins what they leave behind.  Where row tiles are many, every wavefront has
+// one to itself.  Both products are formed transposed,
 // so that a lane's registers belong to one row:
 //   S^T (64 frames x 16 rows) = K q^T     A operand: key rows as they lie in the cache; B operand: the digits of the rows
 //   a lane (row lr = lane % 16, g = lane / 16) then holds the scores of the frames 16 t + 4 g + r of its row
@@ -29,8 +30,9 @@ constexpr int many_waves(int dt, bool packed) { return dt == 8 ? 2 : dt == 2 || 
 struct Place {
   int bh, rt, split;
 };
-__device__ __forceinline__ Place place_of(const CachedGeom &a, int64_t heads) {
-  const int id = static_cast<int>(blockIdx.x);
+__device__ __forceinline__ Place place_of(const CachedGeom &a, int64_t heads, int wave) {
+  const int id = a.own ? static_cast<int>(blockIdx.x) * kWaves + wave : static_cast<int>(blockIdx.x);
+  if (a.own) return Place{id / a.row_tiles, id % a.row_tiles, 0};
   const int64_t lanes = heads * a.splits;   // of row tiles
   int lane, rt;
   if (lanes % 8 == 0) {
@@ -57,7 +59,8 @@ __global__ __launch_bounds__(kThreads, many_waves(DT, PACKED)) void attention_ca
   __shared__ float sm[kWaves][kRows], sl[kWaves][kRows];
   const int tid = static_cast<int>(threadIdx.x), lane = tid & 63, lr = lane & 15, lg = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const Place pl = place_of(a, g.streams * g.kv_heads);
+  const Place pl = place_of(a, g.streams * g.kv_heads, wave);
+  if (a.own && pl.bh >= g.streams * g.kv_heads) return;
   const int h = pl.bh % g.kv_heads;
   const int64_t b = pl.bh / g.kv_heads;
   const StreamFrames f = stream_frames(g, count, a.T, b);
@@ -112,12 +115,12 @@ __global__ __launch_bounds__(kThreads, many_waves(DT, PACKED)) void attention_ca
   };
 
   const uint8_t *const head = g.data + (b * g.kv_heads + h) * g.tiles * static_cast<int64_t>(g.tile_bytes);
-  const int step = a.splits * kWaves, slot_step = step % g.tiles;
+  const int step = a.own ? 1 : a.splits * kWaves, slot_step = step % g.tiles;
   float m = kLowest, l = 0.0f;
   v4f o[DT];                                 // element r of block d: column 16 d + 4 lg + r of this lane's row
 #pragma unroll
   for (int d = 0; d < DT; ++d) o[d] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-  int i = pl.split * kWaves + wave;
+  int i = a.own ? 0 : pl.split * kWaves + wave;
   int slot = tile_slot(tile0 + i, g.tiles);
   if (i < tiles) {
     const uint8_t *const tile = head + static_cast<int64_t>(slot) * g.tile_bytes;
@@ -266,9 +269,23 @@ __global__ __launch_bounds__(kThreads, many_waves(DT, PACKED)) void attention_ca
     load_values(next);
   }
 
-  // the wavefronts' parts of the rows
   l += __shfl_xor(l, 16, 64);
   l += __shfl_xor(l, 32, 64);
+  uint32_t amax = 0u;
+  if (a.own) {
+    const int t = row / a.group;
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;   // nothing seen: zeros
+    float *const to = ctx + ((b * a.T + t) * a.heads + h * a.group + row % a.group) * g.dh;
+#pragma unroll
+    for (int d = 0; d < DT; ++d) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) o[d][r] *= inv;
+      if (t < n) amax = max(amax, put_ctx(to, 16 * d + 4 * lg, g.dh, o[d]));
+    }
+    if (absmax) put_absmax(absmax, amax);
+    return;
+  }
+  // the wavefronts' parts of the rows
   if (lg == 0) {
     sm[wave][lr] = m;
     sl[wave][lr] = l;
@@ -276,7 +293,6 @@ __global__ __launch_bounds__(kThreads, many_waves(DT, PACKED)) void attention_ca
 #pragma unroll
   for (int d = 0; d < DT; ++d) *reinterpret_cast<v4f *>(&so[wave][lr][16 * d + 4 * lg]) = o[d];
   __syncthreads();
-  uint32_t amax = 0u;
   float *const left = part ? part + ((static_cast<int64_t>(pl.bh) * a.row_tiles + pl.rt) * a.splits + pl.split) * P::kFloats : nullptr;
   const int orow = tid >> 4;
   float top = kLowest, sum = 0.0f, weight[kWaves];
@@ -409,6 +425,7 @@ constexpr int64_t kSplitTiles = 24;
 // (splits) that share the tiles of a row tile: a tile for every wavefront at most.
 struct CachedCut {
   int rows, row_tiles, splits;
+  bool own;
   int64_t groups;
 };
 // window: the longest run of frames that a row tile sees
@@ -426,6 +443,10 @@ CachedCut cut_of(const CacheGeom &g, int64_t rows, int64_t window) {
   // window of 5 tiles: 11.0 us in two splits, 9.0 in one), and a wavefront gets two tiles at least.
   const int64_t tiles = cdiv(window, 64) + 1, most = tiles < kSplitTiles ? 1 : tiles / (2 * kWaves), s = want < most ? want : most;
   c.splits = static_cast<int>(s < 1 ? 1 : s);
+  // Where the row tiles are two wavefronts to a SIMD by themselves, nothing is shared: digits are formed once instead of four times and no
+  // parts are joined (2048 row tiles of 64 int8 columns over 3 tiles: 29 us shared, 17 so; over 50: 119, 110).  At half as many a
+  // wavefront stands alone on its SIMD for the whole of a long window (1024 over 8 tiles: 21 and 18; over 20: 30 and 31; over 50: 53 and 63).
+  c.own = c.rows == kRows && (c.groups >= 2048 || (c.groups >= 1024 && tiles <= 10));
   return c;
 }
 
@@ -472,12 +493,13 @@ aqt_status launch_attention_cached(const float *qkv, int64_t T, int heads, const
   const CachedCut cut = cut_of(g, T * a.group, window < c.capacity ? window : c.capacity);
   a.row_tiles = cut.row_tiles;
   a.splits = cut.splits;
+  a.own = cut.own;
   if (absmax) {
     zero_word_kernel<<<1, 64, 0, st>>>(absmax);
     AQT_HIP(hipGetLastError());
   }
   float *const part = cut.splits > 1 ? static_cast<float *>(ws) : nullptr;
-  const unsigned blocks = static_cast<unsigned>(cut.groups * cut.splits);
+  const unsigned blocks = static_cast<unsigned>(cut.own ? cdiv(cut.groups, kWaves) : cut.groups * cut.splits);
   if (cut.rows <= kFewRows) {
     AQT_TRY(launch_attention_cached_few(qkv, g, a, count, ctx, absmax, part, st));
   } else {

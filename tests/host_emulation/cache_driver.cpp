@@ -114,9 +114,9 @@ static void one(int streams, int64_t capacity, int heads, int kv, int dh, int bi
       CachedGeom a{};
       a.T = T; a.ld = cols; a.heads = heads; a.group = group;
       a.left = left; a.right = right; a.scale_log2e = (float)(1.4426950408889634 / sqrt((double)dh));
-      // in tiles of 16 rows, and where they are few, each in its own place; by itself, and joined from three parts
-      for (int form = 0; form < 4; ++form) {
-        const int few_rows = T * group <= kFewRows ? (T * group == 1 ? 1 : T * group == 2 ? 2 : 4) : 0, rows = form & 2 ? few_rows : 16;
+      // in tiles of 16 rows, and where they are few, each in its own place; by itself, and joined from three parts; a tile to a wavefront
+      for (int form = 0; form < 5; ++form) {
+        const int few_rows = T * group <= kFewRows ? (T * group == 1 ? 1 : T * group == 2 ? 2 : 4) : 0, rows = form & 2 ? few_rows : 16, own = form == 4;
         if (rows == 0 || (T > 32 && form == 0)) continue;
         a.splits = form & 1 ? 3 : 1;
         a.row_tiles = (T * group + rows - 1) / rows;
@@ -126,7 +126,8 @@ static void one(int streams, int64_t capacity, int heads, int kv, int dh, int bi
         float *part = splits > 1 ? (float *)aligned_alloc(16, (pf * 4 + 15) / 16 * 16) : nullptr;
         for (size_t i = 0; i < (size_t)streams * T * heads * dh; ++i) ctx[i] = 77.0f;
         uint32_t am = 0;
-        const unsigned grid = (unsigned)(groups * splits);
+        a.own = own;
+        const unsigned grid = (unsigned)(own ? (groups + 3) / 4 : groups * splits);
         run(grid, 256, 0, [&] { attention(g, rows, COLS, qkv, a, count, ctx, &am, part); });
         if (part) run((unsigned)groups, 256, 0, [&] { join(rows, COLS, part, g, a, count, ctx, &am); });
         double worst = 0, largest = 0;
@@ -155,7 +156,7 @@ static void one(int streams, int64_t capacity, int heads, int kv, int dh, int bi
           }
           for (int e = 0; e < dh; ++e) { at_least(worst, fabs(got[e] - ref_o[e]) / mag); at_least(largest, (double)fabsf(got[e])); }
         }
-        printf("  T %d window %d %d splits %d rows %d: worst error / sum of magnitudes %.3g\n", T, left, right, splits, rows, worst);
+        printf("  T %d window %d %d splits %d rows %d own %d: worst error / sum of magnitudes %.3g\n", T, left, right, splits, rows, own, worst);
         if (!(worst < 4e-6)) complain("attention");
         if (__float_as_uint((float)largest) != am) complain("absmax");
         free(ctx); free(part);

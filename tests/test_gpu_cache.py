@@ -266,6 +266,36 @@ def test_attention_over_the_cache(shape, steps, window, scale, ragged):
         cache.advance(T, cd)
 
 
+@pytest.mark.parametrize("streams,capacity,heads,kv,dh,bits,T,window", [
+    (40, 256, 8, 8, 36, 4, 100, (-1, 0)), (24, 192, 16, 4, 64, 8, 90, (70, 3)), (33, 128, 8, 8, 128, 8, 128, (-1, -1)),
+    (35, 64, 8, 8, 20, 3, 121, (9, 0)), (16, 512, 8, 8, 64, 8, 130, (20, 0)), (41, 128, 24, 2, 100, 4, 41, (300, 2))])
+def test_attention_of_many_row_tiles(streams, capacity, heads, kv, dh, bits, T, window):
+    """From 1024 tiles of 16 rows on with a short window, from 2048 on with any: a wavefront has one to itself."""
+    say(streams, capacity, heads, kv, dh, bits, T, window)
+    group = heads // kv
+    assert streams * kv * -(-T * group // 16) >= (1024 if window[0] == 20 else 2048)
+    rng = np.random.default_rng(T)
+    cache, ref = make(streams, capacity, heads, kv, dh, bits)
+    for n in (50, T):
+        rows = new_rows(rng, streams, n, ref.cols)
+        count = rng.integers(-1, n + 2, streams).astype(np.int32)
+        count[:3] = 0, 1, n
+        cd, length = dev(count), host(cache.length)
+        B.aqt_cache_append(dev(rows), cache, n, heads, count=cd)
+        ref.append(rows, n, count)
+        if n == T:
+            start = rng.standard_normal((streams * T, heads * dh)).astype(F)
+            ctx, m = B.aqt_attention_cached_fwd(dev(rows), cache, T, heads, left=window[0], right=window[1], count=cd, ctx=dev(start),
+                                                want_absmax=True)
+            want, tol = ref.attention(rows, T, length, count, *window, start)
+            got = host(ctx)
+            np.testing.assert_array_less(np.abs(got - want), tol + 1e-30)
+            brought = np.concatenate([np.arange(T) < c for c in ref.counts(T, count)])
+            np.testing.assert_array_equal(got[~brought], start[~brought])
+            assert float(m) == np.abs(got[brought]).max()
+        cache.advance(n, cd)
+
+
 @pytest.mark.parametrize("T,group", [(3, 1), (24, 1), (2, 4)])
 def test_a_cache_beyond_4_gib(T, group):
     """The last head's tiles lie behind byte 2^32 of the buffer, the ring's end too."""
