@@ -8,7 +8,6 @@ struct CachedGeom {
   int64_t T, ld;            // new rows per stream, columns of a row
   int heads, group;         // query heads, and how many of them share a key / value head
   int row_tiles, splits;
-  int own;                  // every wavefront has a row tile to itself (attention_cached.hip; splits is 1 then)
   int64_t left, right;      // negative: no limit
   float scale_log2e;
 };

@@ -24,15 +24,18 @@ namespace {
 constexpr int kRows = 16;                 // rows of a workgroup
 // Wavefronts per SIMD that the kernel's registers are shared out to, without spills (dt: blocks of 16 head columns).
 constexpr int many_waves(int dt, bool packed) { return dt == 8 ? 2 : dt == 2 || packed ? 4 : 3; }
+// A row tile to a wavefront: fewer bytes of LDS (8192 row tiles of 128 int4 columns over 3 tiles: 95 us with two wavefronts, 90 so).
+constexpr int own_waves(int dt, bool packed) { return dt == 8 && packed ? 3 : many_waves(dt, packed); }
 
 // The workgroup's place: (stream and head, row tile, split).  The row tiles of a split read the same codes; workgroup ids eight apart run
 // on one XCD, so that with a multiple of eight of them the row tiles of a split are given to one XCD's L2.
 struct Place {
   int bh, rt, split;
 };
+template <bool OWN>
 __device__ __forceinline__ Place place_of(const CachedGeom &a, int64_t heads, int wave) {
-  const int id = a.own ? static_cast<int>(blockIdx.x) * kWaves + wave : static_cast<int>(blockIdx.x);
-  if (a.own) return Place{id / a.row_tiles, id % a.row_tiles, 0};
+  const int id = OWN ? static_cast<int>(blockIdx.x) * kWaves + wave : static_cast<int>(blockIdx.x);
+  if constexpr (OWN) return Place{id / a.row_tiles, id % a.row_tiles, 0};
   const int64_t lanes = heads * a.splits;   // of row tiles
   int lane, rt;
   if (lanes % 8 == 0) {
@@ -45,9 +48,9 @@ __device__ __forceinline__ Place place_of(const CachedGeom &a, int64_t heads, in
   return Place{lane / a.splits, rt, lane % a.splits};
 }
 
-// DT: blocks of 16 head columns that a workgroup holds (2, 4 or 8)
-template <int DT, bool PACKED>
-__global__ __launch_bounds__(kThreads, many_waves(DT, PACKED)) void attention_cached_kernel(const float *__restrict__ qkv, CacheGeom g, CachedGeom a,
+// DT: blocks of 16 head columns that a workgroup holds (2, 4 or 8); OWN: every wavefront has a row tile to itself (splits is 1 then)
+template <int DT, bool PACKED, bool OWN>
+__global__ __launch_bounds__(kThreads, OWN ? own_waves(DT, PACKED) : many_waves(DT, PACKED)) void attention_cached_kernel(const float *__restrict__ qkv, CacheGeom g, CachedGeom a,
                                                                        const int32_t *__restrict__ count, float *__restrict__ ctx,
                                                                        uint32_t *__restrict__ absmax, float *__restrict__ part) {
   constexpr int KS = DT == 8 ? 2 : 1;        // steps of 64 head columns
@@ -59,8 +62,8 @@ __global__ __launch_bounds__(kThreads, many_waves(DT, PACKED)) void attention_ca
   __shared__ float sm[kWaves][kRows], sl[kWaves][kRows];
   const int tid = static_cast<int>(threadIdx.x), lane = tid & 63, lr = lane & 15, lg = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const Place pl = place_of(a, g.streams * g.kv_heads, wave);
-  if (a.own && pl.bh >= g.streams * g.kv_heads) return;
+  const Place pl = place_of<OWN>(a, g.streams * g.kv_heads, wave);
+  if (OWN && pl.bh >= g.streams * g.kv_heads) return;
   const int h = pl.bh % g.kv_heads;
   const int64_t b = pl.bh / g.kv_heads;
   const StreamFrames f = stream_frames(g, count, a.T, b);
@@ -115,12 +118,12 @@ __global__ __launch_bounds__(kThreads, many_waves(DT, PACKED)) void attention_ca
   };
 
   const uint8_t *const head = g.data + (b * g.kv_heads + h) * g.tiles * static_cast<int64_t>(g.tile_bytes);
-  const int step = a.own ? 1 : a.splits * kWaves, slot_step = step % g.tiles;
+  const int step = OWN ? 1 : a.splits * kWaves, slot_step = step % g.tiles;
   float m = kLowest, l = 0.0f;
   v4f o[DT];                                 // element r of block d: column 16 d + 4 lg + r of this lane's row
 #pragma unroll
   for (int d = 0; d < DT; ++d) o[d] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
-  int i = a.own ? 0 : pl.split * kWaves + wave;
+  int i = OWN ? 0 : pl.split * kWaves + wave;
   int slot = tile_slot(tile0 + i, g.tiles);
   if (i < tiles) {
     const uint8_t *const tile = head + static_cast<int64_t>(slot) * g.tile_bytes;
@@ -272,7 +275,7 @@ __global__ __launch_bounds__(kThreads, many_waves(DT, PACKED)) void attention_ca
   l += __shfl_xor(l, 16, 64);
   l += __shfl_xor(l, 32, 64);
   uint32_t amax = 0u;
-  if (a.own) {
+  if constexpr (OWN) {
     const int t = row / a.group;
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;   // nothing seen: zeros
     float *const to = ctx + ((b * a.T + t) * a.heads + h * a.group + row % a.group) * g.dh;
@@ -444,7 +447,7 @@ CachedCut cut_of(const CacheGeom &g, int64_t rows, int64_t window) {
   const int64_t tiles = cdiv(window, 64) + 1, most = tiles < kSplitTiles ? 1 : tiles / (2 * kWaves), s = want < most ? want : most;
   c.splits = static_cast<int>(s < 1 ? 1 : s);
   // Where the row tiles are two wavefronts to a SIMD by themselves, nothing is shared: digits are formed once instead of four times and no
-  // parts are joined (2048 row tiles of 64 int8 columns over 3 tiles: 29 us shared, 17 so; over 50: 119, 110).  At half as many a
+  // parts are joined (2048 row tiles of 64 int8 columns over 3 tiles: 29 us shared, 18 so; over 50: 119, 110).  At half as many a
   // wavefront stands alone on its SIMD for the whole of a long window (1024 over 8 tiles: 21 and 18; over 20: 30 and 31; over 50: 53 and 63).
   c.own = c.rows == kRows && (c.groups >= 2048 || (c.groups >= 1024 && tiles <= 10));
   return c;
@@ -462,6 +465,16 @@ void launch_join(const float *part, const CacheGeom &g, const CachedGeom &a, con
               : g.dh <= 64 ? attention_cached_join_kernel<ROWS, 64>
                            : attention_cached_join_kernel<ROWS, 128>;
   join<<<groups, kThreads, 0, st>>>(part, g, a, count, ctx, absmax);
+}
+
+template <bool OWN>
+auto many_kernel(int dh, bool packed) {
+  return packed ? (dh <= 32   ? attention_cached_kernel<2, true, OWN>
+                   : dh <= 64 ? attention_cached_kernel<4, true, OWN>
+                              : attention_cached_kernel<8, true, OWN>)
+                : (dh <= 32   ? attention_cached_kernel<2, false, OWN>
+                   : dh <= 64 ? attention_cached_kernel<4, false, OWN>
+                              : attention_cached_kernel<8, false, OWN>);
 }
 
 }  // namespace
@@ -493,7 +506,6 @@ aqt_status launch_attention_cached(const float *qkv, int64_t T, int heads, const
   const CachedCut cut = cut_of(g, T * a.group, window < c.capacity ? window : c.capacity);
   a.row_tiles = cut.row_tiles;
   a.splits = cut.splits;
-  a.own = cut.own;
   if (absmax) {
     zero_word_kernel<<<1, 64, 0, st>>>(absmax);
     AQT_HIP(hipGetLastError());
@@ -503,12 +515,7 @@ aqt_status launch_attention_cached(const float *qkv, int64_t T, int heads, const
   if (cut.rows <= kFewRows) {
     AQT_TRY(launch_attention_cached_few(qkv, g, a, count, ctx, absmax, part, st));
   } else {
-    auto kern = g.packed ? (c.dh <= 32   ? attention_cached_kernel<2, true>
-                            : c.dh <= 64 ? attention_cached_kernel<4, true>
-                                         : attention_cached_kernel<8, true>)
-                         : (c.dh <= 32   ? attention_cached_kernel<2, false>
-                            : c.dh <= 64 ? attention_cached_kernel<4, false>
-                                         : attention_cached_kernel<8, false>);
+    const auto kern = cut.own ? many_kernel<true>(c.dh, g.packed) : many_kernel<false>(c.dh, g.packed);
     kern<<<blocks, kThreads, 0, st>>>(qkv, g, a, count, ctx, absmax, part);
     AQT_HIP(hipGetLastError());
   }

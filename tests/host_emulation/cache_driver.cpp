@@ -27,15 +27,16 @@ template <int L, bool VEC> static void read_(unsigned grid, const CacheGeom &g, 
   run(grid, 256, 0, [&] { cache_::cache_read_kernel<L, VEC>(g, pend, count, first, n, run_, per, k, v); });
 }
 
-template <int DT, bool PACKED> static void attention_as(const CacheGeom &g, int rows, const float *qkv, const CachedGeom &a, const int32_t *count, float *ctx, uint32_t *am, float *part) {
-  if (rows == 16) attend::attention_cached_kernel<DT, PACKED>(qkv, g, a, count, ctx, am, part);
+template <int DT, bool PACKED> static void attention_as(const CacheGeom &g, int rows, bool own, const float *qkv, const CachedGeom &a, const int32_t *count, float *ctx, uint32_t *am, float *part) {
+  if (own) attend::attention_cached_kernel<DT, PACKED, true>(qkv, g, a, count, ctx, am, part);
+  else if (rows == 16) attend::attention_cached_kernel<DT, PACKED, false>(qkv, g, a, count, ctx, am, part);
   else if (rows == 1) few::attention_cached_few_kernel<DT, PACKED, 1>(qkv, g, a, count, ctx, am, part);
   else if (rows == 2) few::attention_cached_few_kernel<DT, PACKED, 2>(qkv, g, a, count, ctx, am, part);
   else few::attention_cached_few_kernel<DT, PACKED, 4>(qkv, g, a, count, ctx, am, part);
 }
-static void attention(const CacheGeom &g, int rows, int cols, const float *qkv, const CachedGeom &a, const int32_t *count, float *ctx, uint32_t *am, float *part) {
-  if (g.packed) (cols == 32 ? attention_as<2, true> : cols == 64 ? attention_as<4, true> : attention_as<8, true>)(g, rows, qkv, a, count, ctx, am, part);
-  else (cols == 32 ? attention_as<2, false> : cols == 64 ? attention_as<4, false> : attention_as<8, false>)(g, rows, qkv, a, count, ctx, am, part);
+static void attention(const CacheGeom &g, int rows, bool own, int cols, const float *qkv, const CachedGeom &a, const int32_t *count, float *ctx, uint32_t *am, float *part) {
+  if (g.packed) (cols == 32 ? attention_as<2, true> : cols == 64 ? attention_as<4, true> : attention_as<8, true>)(g, rows, own, qkv, a, count, ctx, am, part);
+  else (cols == 32 ? attention_as<2, false> : cols == 64 ? attention_as<4, false> : attention_as<8, false>)(g, rows, own, qkv, a, count, ctx, am, part);
 }
 template <int ROWS> static void join_as(int cols, const float *part, const CacheGeom &g, const CachedGeom &a, const int32_t *count, float *ctx, uint32_t *am) {
   if (cols == 32) attend::attention_cached_join_kernel<ROWS, 32>(part, g, a, count, ctx, am);
@@ -116,7 +117,8 @@ static void one(int streams, int64_t capacity, int heads, int kv, int dh, int bi
       a.left = left; a.right = right; a.scale_log2e = (float)(1.4426950408889634 / sqrt((double)dh));
       // in tiles of 16 rows, and where they are few, each in its own place; by itself, and joined from three parts; a tile to a wavefront
       for (int form = 0; form < 5; ++form) {
-        const int few_rows = T * group <= kFewRows ? (T * group == 1 ? 1 : T * group == 2 ? 2 : 4) : 0, rows = form & 2 ? few_rows : 16, own = form == 4;
+        const int few_rows = T * group <= kFewRows ? (T * group == 1 ? 1 : T * group == 2 ? 2 : 4) : 0, rows = form & 2 ? few_rows : 16;
+        const bool own = form == 4;
         if (rows == 0 || (T > 32 && form == 0)) continue;
         a.splits = form & 1 ? 3 : 1;
         a.row_tiles = (T * group + rows - 1) / rows;
@@ -126,9 +128,8 @@ static void one(int streams, int64_t capacity, int heads, int kv, int dh, int bi
         float *part = splits > 1 ? (float *)aligned_alloc(16, (pf * 4 + 15) / 16 * 16) : nullptr;
         for (size_t i = 0; i < (size_t)streams * T * heads * dh; ++i) ctx[i] = 77.0f;
         uint32_t am = 0;
-        a.own = own;
         const unsigned grid = (unsigned)(own ? (groups + 3) / 4 : groups * splits);
-        run(grid, 256, 0, [&] { attention(g, rows, COLS, qkv, a, count, ctx, &am, part); });
+        run(grid, 256, 0, [&] { attention(g, rows, own, COLS, qkv, a, count, ctx, &am, part); });
         if (part) run((unsigned)groups, 256, 0, [&] { join(rows, COLS, part, g, a, count, ctx, &am); });
         double worst = 0, largest = 0;
         for (int b = 0; b < streams; ++b) for (int t = 0; t < T; ++t) for (int h = 0; h < heads; ++h) {
