@@ -224,21 +224,33 @@ __global__ __launch_bounds__(kThreads, OWN ? own_waves(DT, PACKED) : many_waves(
 #pragma unroll
           for (int r = 0; r < 4; ++r) o[d][r] *= alpha;
       }
-      // Probabilities, and their digits times the values' scales: relative to the largest probability times the largest scale, a
-      // bound of the largest weight.
-      const float top = fmaxf(__builtin_amdgcn_exp2f(mx - m) * vs_top, 0x1p-100f);
-      const float to = kDigits * __builtin_amdgcn_rcpf(top);
-      unit = top * (1.0f / kDigits) * (PACKED ? 0.0625f : 1.0f);
+      // Probabilities, and weights: probabilities times the values' scales.  The weights' digits are relative to the largest probability
+      // times the largest scale, a bound of the largest weight; where a row's weights all lie under a quarter of it (most of the
+      // probability meets a small value, or the large value is not the row's to see), to the row's largest weight itself, which takes
+      // moves between lanes.  So the largest of a row and tile is an integer of 2^21 at least.  (32 streams, 512 new
+      // frames and no others, 8 heads of 64, int8: 68.5 us without the look at the weights, 72 so; other forms and sizes: equal.)
+      float most = 0.0f;
 #pragma unroll
       for (int t = 0; t < 4; ++t) {
         const v4f vs4 = *reinterpret_cast<const v4f *>(&sc[64 + 16 * t + 4 * lg]);
-        uint32_t w[4];
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const float e = __builtin_amdgcn_exp2f(s[4 * t + r] - m);
           l += e;
-          w[r] = weight_bits(e, vs4[r] * to);
+          s[4 * t + r] = e * vs4[r];
+          most = fmaxf(most, s[4 * t + r]);
         }
+      }
+      float top = __builtin_amdgcn_exp2f(mx - m) * vs_top;
+      if (!rows_all(most >= 0.25f * top)) top = max_of_groups(most);
+      top = fmaxf(top, 0x1p-100f);
+      const float to = kDigits * __builtin_amdgcn_rcpf(top);
+      unit = top * (1.0f / kDigits) * (PACKED ? 0.0625f : 1.0f);
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        uint32_t w[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) w[r] = weight_bits(s[4 * t + r], to);
         int d0, d1, d2;
         weight_digits4(w, d0, d1, d2);
         p[0][t] = d0;

@@ -7,8 +7,9 @@
 //                                  of lanes then hold the scores of all 16; group g keeps those of the g-th 16
 //   O (rows x dh) = P V            A operand: the probabilities' digits, through LDS (a byte per digit); B operand: value rows.  Again
 //                                  every group holds all of 16 columns, and group g keeps the g-th 16
-// The probabilities' digits are relative to exp2(largest score - running maximum) times the tile's largest value scale: a bound of
-// the tile's largest weight that takes one maximum over the wavefront per row and tile.
+// The weights' digits are relative to exp2(largest score - running maximum) times the tile's largest value scale, a bound of the
+// tile's largest weight that takes one maximum over the wavefront per row and tile; where a row's weights all lie under a quarter
+// of it, to the row's largest weight itself.
 #include "attention_cached.h"
 
 namespace aqt {
@@ -188,7 +189,8 @@ __global__ __launch_bounds__(kThreads, few_waves(DT, PACKED, R)) void attention_
     }
     vs = any ? vs : 0.0f;
     const float vs_top = wave_max_positive(vs);
-    float alpha[R], unit[R];
+    float alpha[R], unit[R], weight[R], top[R];
+    bool near = true;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       const float mx = wave_max_signed(see[r] ? s[r] : kLowest), mnew = fmaxf(m[r], mx);
@@ -196,9 +198,19 @@ __global__ __launch_bounds__(kThreads, few_waves(DT, PACKED, R)) void attention_
       m[r] = mnew;
       const float p = see[r] ? __builtin_amdgcn_exp2f(s[r] - mnew) : 0.0f;
       l[r] = fmaf(l[r], alpha[r], p);
-      const float top = fmaxf(__builtin_amdgcn_exp2f(mx - mnew) * vs_top, 0x1p-100f);
-      unit[r] = top * (1.0f / kDigits) * (PACKED ? 0.0625f : 1.0f);
-      const uint32_t u = weight_bits(p, vs * (kDigits * __builtin_amdgcn_rcpf(top))) ^ 0x00008080u;
+      weight[r] = p * vs;
+      top[r] = __builtin_amdgcn_exp2f(mx - mnew) * vs_top;
+      near = near && __any(weight[r] >= 0.25f * top[r]);
+    }
+    if (!near) {
+#pragma unroll
+      for (int r = 0; r < R; ++r) top[r] = wave_max_positive(weight[r]);
+    }
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+      top[r] = fmaxf(top[r], 0x1p-100f);
+      unit[r] = top[r] * (1.0f / kDigits) * (PACKED ? 0.0625f : 1.0f);
+      const uint32_t u = weight_bits(weight[r], kDigits * __builtin_amdgcn_rcpf(top[r])) ^ 0x00008080u;
       put[(2 * R + r) * 64] = static_cast<uint8_t>(u);
       put[(R + r) * 64] = static_cast<uint8_t>(u >> 8);
       put[r * 64] = static_cast<uint8_t>(u >> 16);

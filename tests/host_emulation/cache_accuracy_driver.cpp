@@ -1,0 +1,179 @@
+// Driver of the host emulation of the attention over the quantized cache for values, keys and queries of very different sizes: one
+// stream, one key / value head, every form of the kernels, against float64 loops.  It follows cache_driver.cpp's helpers (quantized,
+// append, attention, join) in the same file, which the test puts in front.
+namespace aqt {
+constexpr double kU = 0x1p-24;
+
+struct Rows {   // of one stream: `frames` rows of group queries, one key, one value; the last T are the call's own
+  int frames, T, group, dh, bits;
+  std::vector<float> x;
+  int cols() const { return (group + 2) * dh; }
+  float *query(int j, int h) { return &x[(size_t)j * cols() + h * dh]; }
+  float *key(int j) { return &x[(size_t)j * cols() + group * dh]; }
+  float *value(int j) { return &x[(size_t)j * cols() + (group + 1) * dh]; }
+};
+static Rows make_rows(int frames, int T, int group, int dh, int bits) {
+  Rows r{frames, T, group, dh, bits, {}};
+  r.x.resize((size_t)frames * r.cols());
+  for (float &v : r.x) v = 2.0f * uniform();
+  return r;
+}
+
+struct Cached {   // the rows in their cache
+  CacheGeom g;
+  int64_t length;
+  std::vector<std::vector<double>> k, v;   // code * scale
+};
+static void fill(Cached &c, Rows &r) {
+  aqt_cache shape{};
+  shape.streams = 1; shape.capacity = (r.frames + 63) / 64 * 64; shape.kv_heads = 1; shape.dh = r.dh; shape.bits = r.bits;
+  c.g = cache_geom(shape);
+  const size_t bytes = (size_t)c.g.tiles * c.g.tile_bytes;
+  c.g.data = (uint8_t *)aligned_alloc(64, (bytes + 63) / 64 * 64);
+  memset(c.g.data, 0xFF, bytes);
+  c.length = 0;
+  c.g.length = &c.length;
+  const int L = cache_::lanes_of(r.dh), per = (int)cache_::cut_of(c.g, r.frames).blocks;
+  const bool vec = r.dh % 4 == 0;
+  auto ap = L == 4 ? (vec ? append<4, true> : append<4, false>) : L == 8 ? (vec ? append<8, true> : append<8, false>) : (vec ? append<16, true> : append<16, false>);
+  ap((unsigned)per, r.x.data(), c.g, r.frames, r.group, nullptr, cache_::cut_of(c.g, r.frames).log2_run, per, nullptr);
+  c.length = r.frames - r.T;
+  for (int j = 0; j < r.frames; ++j) {
+    std::vector<double> k(r.dh), v(r.dh);
+    quantized(r.key(j), r.dh, c.g.qmax, k, 0);
+    quantized(r.value(j), r.dh, c.g.qmax, v, 0);
+    c.k.push_back(k); c.v.push_back(v);
+  }
+}
+
+// ctx of the T * group rows, in one of the five forms: 0 / 1 tiles of 16 rows, by themselves / from three splits; 2 / 3 few rows; 4 a
+// wavefront to every tile.  Empty where the form does not take so many rows.
+static std::vector<float> attend_form(Cached &c, Rows &r, int64_t left, int64_t right, int form) {
+  const int n = r.T * r.group, few_rows = n <= kFewRows ? (n == 1 ? 1 : n == 2 ? 2 : 4) : 0, rows = form & 2 ? few_rows : 16;
+  if (rows == 0) return {};
+  CachedGeom a{};
+  a.T = r.T; a.ld = r.cols(); a.heads = r.group; a.group = r.group; a.left = left; a.right = right;
+  a.scale_log2e = (float)(1.4426950408889634 / sqrt((double)r.dh));
+  a.splits = form & 1 ? 3 : 1;
+  a.row_tiles = (n + rows - 1) / rows;
+  const int COLS = attend::cols_of(r.dh);
+  const size_t pf = (size_t)a.row_tiles * a.splits * ((rows * COLS + 2 * rows + 3) / 4 * 4);
+  float *part = a.splits > 1 ? (float *)aligned_alloc(16, (pf * 4 + 15) / 16 * 16) : nullptr;
+  float *ctx = (float *)malloc((size_t)n * r.dh * 4);
+  const float *qkv = r.x.data() + (size_t)(r.frames - r.T) * r.cols();
+  const unsigned grid = (unsigned)(form == 4 ? (a.row_tiles + 3) / 4 : a.row_tiles * a.splits);
+  run(grid, 256, 0, [&] { attention(c.g, rows, form == 4, COLS, qkv, a, nullptr, ctx, nullptr, part); });
+  if (part) run((unsigned)a.row_tiles, 256, 0, [&] { join(rows, COLS, part, c.g, a, nullptr, ctx, nullptr); });
+  std::vector<float> out(ctx, ctx + (size_t)n * r.dh);
+  free(ctx); free(part);
+  return out;
+}
+
+// One row in float64, and its tolerance relative to the sum of weights times the frames' largest values.  A score: the query's digits
+// are off by half a unit of its largest column over 2^23, and eight roundings.  A weight: an integer of which the largest of a tile is
+// 2^21 at least, so half a unit is 4 U of it, for each of 64 frames; four roundings for every tile, the sum of weights sixteen.
+struct Want { std::vector<double> o; double mag, tol; };
+static Want want_of(const Cached &c, Rows &r, int t, int h, int64_t left, int64_t right) {
+  const int64_t f = r.frames - r.T + t, lo = left < 0 ? 0 : std::max<int64_t>(0, f - left), hi = right < 0 ? r.frames - 1 : std::min<int64_t>(r.frames - 1, f + right);
+  const float *q = r.query((int)f, h);
+  double qmax = 0, top = -1e300, reach = 0, largest = 0, spread = 0, sum = 0;
+  for (int e = 0; e < r.dh; ++e) qmax = std::max(qmax, (double)fabsf(q[e]));
+  std::vector<double> s;
+  for (int64_t j = lo; j <= hi; ++j) {
+    double d = 0, m = 0;
+    for (int e = 0; e < r.dh; ++e) { d += c.k[j][e] * q[e]; m += fabs(c.k[j][e]); }
+    s.push_back(d / sqrt((double)r.dh));
+    top = std::max(top, s.back()); largest = std::max(largest, fabs(s.back())); reach = std::max(reach, qmax * m / sqrt((double)r.dh));
+  }
+  for (double x : s) { spread = std::max(spread, top - x); sum += exp(x - top); }
+  Want w{std::vector<double>(r.dh, 0.0), 1e-30, 0};
+  for (int64_t j = lo; j <= hi; ++j) {
+    const double p = exp(s[j - lo] - top) / sum;
+    double most = 0;
+    for (int e = 0; e < r.dh; ++e) { w.o[e] += p * c.v[j][e]; most = std::max(most, fabs(c.v[j][e])); }
+    w.mag += p * most;
+  }
+  // (frames whose score lies more than 110 below the largest weigh nothing, and their roundings neither)
+  const double e = kU * reach + 8 * kU * largest + kU * (std::min(spread, 110.0) + 8);
+  w.tol = 2 * e + (256 + 20 * ((double)(hi - lo + 1) / 64 + 2) + 30) * kU;
+  return w;
+}
+
+static void compare(Rows &r, int64_t left, int64_t right, const char *what) {
+  printf("%s: %d frames, %d new, group %d, dh %d, bits %d\n", what, r.frames, r.T, r.group, r.dh, r.bits); fflush(stdout);
+  Cached c;
+  fill(c, r);
+  for (int form = 0; form < 5; ++form) {
+    const std::vector<float> got = attend_form(c, r, left, right, form);
+    if (got.empty()) continue;
+    double worst = 0, part = 0;
+    for (int t = 0; t < r.T; ++t) for (int h = 0; h < r.group; ++h) {
+      const Want w = want_of(c, r, t, h, left, right);
+      for (int e = 0; e < r.dh; ++e) {
+        const double d = fabs(got[((size_t)t * r.group + h) * r.dh + e] - w.o[e]) / w.mag;
+        at_least(worst, d); at_least(part, d / w.tol);
+      }
+    }
+    printf("  form %d: worst error %.3g, %.3g of its tolerance\n", form, worst, part);
+    if (!(part <= 1.0)) complain(what);
+  }
+  free(c.g.data);
+}
+
+// The first frame draws `lift` more than the others and has values of `size`: most of the weight, and next to no value.
+static void sink(int T, int group, int dh, int bits, double lift, float size) {
+  Rows r = make_rows(200, T, group, dh, bits);
+  for (int j = 0; j < r.frames; ++j) {
+    for (int h = 0; h < group; ++h) r.query(j, h)[0] = 3.0f;
+    r.key(j)[0] = 0.0f;
+  }
+  for (int e = 0; e < dh; ++e) { r.key(0)[e] = 0.0f; r.value(0)[e] *= size; }
+  r.key(0)[0] = (float)(lift * sqrt((double)dh) / 3.0);
+  char what[64];
+  snprintf(what, sizeof what, "sink + %g, value x %g", lift, size);
+  compare(r, -1, 0, what);
+}
+// The call's last frame, which the rows in front of it do not see, and one that nobody listens to have values `size` times the others'.
+static void large_elsewhere(int T, int group, int dh, int bits, float size) {
+  Rows r = make_rows(130, T, group, dh, bits);
+  for (int j = 0; j < r.frames; ++j) {
+    for (int h = 0; h < group; ++h) r.query(j, h)[0] = 4.0f;
+    r.key(j)[0] = 0.0f;
+  }
+  r.key(r.frames - 9)[0] = -30.0f * sqrtf((float)dh);   // score -120: a weight of nothing
+  for (int e = 0; e < dh; ++e) { r.value(r.frames - 1)[e] *= size; r.value(r.frames - 9)[e] *= size; }
+  char what[64];
+  snprintf(what, sizeof what, "values x %g where no weight is", size);
+  compare(r, -1, 0, what);
+}
+static void drawn_sizes(int T, int group, int dh, int bits) {
+  Rows r = make_rows(200, T, group, dh, bits);
+  for (int j = 0; j < r.frames; ++j) {
+    const float size = exp2f(-10.0f + 10.0f * uniform());
+    for (int e = 0; e < dh; ++e) r.value(j)[e] *= size;
+    for (int h = 0; h < group; ++h) for (int e = 0; e < dh; ++e) r.query(j, h)[e] *= 3.0f;
+  }
+  compare(r, -1, 0, "values of 2^-20 to 1");
+}
+static void weights() {
+  for (float size : {0.1f, 0.01f, 0.0f}) sink(1, 1, 64, 8, 10, size);
+  sink(1, 2, 64, 8, 14, 0.01f);
+  sink(4, 1, 64, 8, 20, 0.0f);
+  sink(2, 4, 128, 4, 20, 0.0f);
+  sink(3, 1, 36, 4, 20, 0.0f);
+  sink(17, 1, 20, 8, 20, 0.0f);
+  for (float size : {1e3f, 1e7f}) { large_elsewhere(4, 1, 64, 8, size); large_elsewhere(12, 1, 64, 8, size); }
+  large_elsewhere(2, 2, 128, 4, 1e5f);
+  large_elsewhere(2, 10, 32, 4, 1e5f);
+  drawn_sizes(2, 1, 64, 8);
+  drawn_sizes(5, 2, 64, 4);
+}
+}  // namespace aqt
+int main(int argc, char **argv) {
+  using namespace aqt;
+  const std::string what = argc > 1 ? argv[1] : "";
+  if (what == "weights") weights();
+  else complain("no such test");
+  printf(bad ? "MISMATCH\n" : "ok\n");
+  return bad;
+}

@@ -1,0 +1,108 @@
+"""The attention over the quantized cache on what a cache of real streams holds: frames whose values, keys and queries are of very
+different sizes, in every form of the kernels, against float64 on what the codes stand for."""
+import numpy as np
+import pytest
+
+from paper_2203_15952_amd import binding as B
+from test_gpu_cache import F, U, dev, host, make, say
+
+pytestmark = pytest.mark.gpu
+
+# streams, capacity, heads, kv_heads, dh, bits, frames, new ones of them: a few rows, tiles of sixteen, both from several splits, and a
+# wavefront to every tile
+FORMS = [(1, 256, 1, 1, 64, 8, 200, 1), (2, 256, 4, 2, 36, 4, 200, 2), (1, 256, 8, 2, 128, 8, 200, 1), (2, 192, 2, 2, 20, 8, 180, 17),
+         (1, 256, 12, 1, 128, 4, 200, 2), (1, 4096, 2, 2, 64, 8, 4000, 2), (1, 4096, 3, 1, 80, 4, 4000, 20), (33, 128, 8, 8, 64, 8, 128, 128),
+         (16, 128, 8, 4, 100, 4, 120, 120)]
+
+
+def expected(ref, rows, T, left, right):
+    """ctx of the last T frames in float64, and what an output may be off by.  A score: the query's digits are off by half a unit of
+    its largest column over 2^23, so by U max|q| sum|k| / sqrt(dh), and eight roundings of it and of its distance from the largest
+    (a frame 110 below it weighs nothing, and its roundings neither); twice that in the quotient.  A weight, probability times scale: an
+    integer of which the largest of a tile is 2^21 at least, so half a unit is 4 U of it, for each of 64 frames; four roundings for
+    every tile, the sum of weights sixteen.  Relative to the sum of the weights times the frames' largest values."""
+    x = rows.reshape(ref.n, T, -1, ref.dh)
+    out, tol = np.zeros((ref.n, T, ref.heads, ref.dh)), np.zeros((ref.n, T, ref.heads, 1))
+    g = ref.heads // ref.kv
+    for b in range(ref.n):
+        end = ref.end(b)
+        k, v = (np.repeat(a[b].astype(np.float64), g, axis=1).transpose(1, 0, 2) for a in (ref.k, ref.v))    # [heads, frames, dh]
+        q = x[b, :, :ref.heads].astype(np.float64).transpose(1, 0, 2)
+        f, j = end - T + np.arange(T), np.arange(end)
+        seen = (j[None] >= f[:, None] - left if left >= 0 else np.ones((T, end), bool)) & (j[None] <= f[:, None] + right if right >= 0 else True)
+        s = q @ k.transpose(0, 2, 1) / np.sqrt(ref.dh)
+        score = np.where(seen[None], s, -np.inf)
+        p = np.exp(score - score.max(2, keepdims=True))
+        p /= p.sum(2, keepdims=True)
+        out[b] = (p @ v).transpose(1, 0, 2)
+        mag = (p * np.abs(v).max(2)[:, None]).sum(2)
+        reach = np.abs(q).max(2) * (np.where(seen[None], np.abs(k).sum(2)[:, None], 0).max(2)) / np.sqrt(ref.dh)
+        spread = np.minimum(score.max(2) - np.where(seen[None], s, np.inf).min(2), 110.0)
+        e = U * reach + 8 * U * np.where(seen[None], np.abs(s), 0).max(2) + U * (spread + 8)
+        tol[b, :, :, 0] = ((2 * e + (256 + 20 * (end / 64 + 2) + 30) * U) * mag).T
+    return out.reshape(ref.n * T, -1), np.broadcast_to(tol, out.shape).reshape(ref.n * T, -1)
+
+
+def run(form, change, left=-1, right=0):
+    """The form's frames, after change(queries, keys, values) in place ([streams, frames, heads, dh] each), through the cache."""
+    streams, capacity, heads, kv, dh, bits, n, T = form
+    rng = np.random.default_rng(n + T + dh)
+    rows = (2 * rng.uniform(-1, 1, (streams, n, heads + 2 * kv, dh))).astype(F)
+    change(rows[:, :, :heads], rows[:, :, heads:heads + kv], rows[:, :, heads + kv:])
+    cache, ref = make(streams, capacity, heads, kv, dh, bits)
+    if n > T:
+        old = np.ascontiguousarray(rows[:, :n - T]).reshape(-1, ref.cols)
+        B.aqt_cache_append(dev(old), cache, n - T, heads)
+        ref.append(old, n - T)
+        cache.advance(n - T)
+    new = np.ascontiguousarray(rows[:, n - T:]).reshape(-1, ref.cols)
+    B.aqt_cache_append(dev(new), cache, T, heads)
+    ref.append(new, T)
+    return host(B.aqt_attention_cached_fwd(dev(new), cache, T, heads, left=left, right=right)[0]), ref, new
+
+
+def compare(form, change, left=-1, right=0):
+    got, ref, new = run(form, change, left, right)
+    want, tol = expected(ref, new, form[-1], left, right)
+    err = np.abs(got - want)
+    say("  worst", (err / (tol + 1e-30)).max(), "of its tolerance")
+    assert (err <= tol + 1e-30).all()
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("lift,size", [(10, 0.03), (14, 0.0), (20, 0.0)])
+def test_most_of_the_weight_and_next_to_no_value(form, lift, size):
+    """A first frame that draws `lift` more than the others, as attention sinks do."""
+    say("sink", form, lift, size)
+
+    def change(q, k, v):
+        q[..., 0], k[..., 0], k[:, 0] = 3.0, 0.0, 0.0
+        k[:, 0, :, 0] = lift * np.sqrt(form[4]) / 3
+        v[:, 0] *= F(size)
+    compare(form, change)
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("size", [1e3, 1e5, 1e7])
+def test_large_values_where_no_weight_is(form, size):
+    """The call's last frame, which the rows in front of it do not see, and one that nobody listens to."""
+    say("large", form, size)
+
+    def change(q, k, v):
+        q[..., 0], k[..., 0] = 4.0, 0.0
+        k[:, -5, :, 0] = -30 * np.sqrt(form[4])
+        v[:, -1] *= F(size)
+        v[:, -5] *= F(size)
+    compare(form, change)
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("window", [(-1, -1), (50, 2)])
+def test_values_of_all_sizes(form, window):
+    say("sizes", form, window)
+    rng = np.random.default_rng(form[-1])
+
+    def change(q, k, v):
+        q *= F(3)
+        v *= np.exp2(rng.uniform(-20, 0, v.shape[:2])).astype(F)[:, :, None, None]
+    compare(form, change, *window)
