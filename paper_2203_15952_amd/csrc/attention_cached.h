@@ -65,11 +65,11 @@ __device__ __forceinline__ float max_of_groups(float v) {   // over the four lan
   return fmaxf(v, __shfl_xor(v, 32, 64));
 }
 
-// Whether each of the 16 rows has it in one of its four lanes at least.
-__device__ __forceinline__ bool rows_all(bool has) {
+// The rows, of 16, that have it in one of their four lanes.
+__device__ __forceinline__ uint32_t rows_with(bool has) {
   uint64_t b = __ballot(has);
   b |= b >> 32;
-  return ((b | b >> 16) & 0xFFFFu) == 0xFFFFu;
+  return static_cast<uint32_t>(b | b >> 16) & 0xFFFFu;
 }
 
 // The largest of a wavefront's 64 words.  (The steps fuse with the moves between lanes, as they do not for float32.)

@@ -242,7 +242,11 @@ __global__ __launch_bounds__(kThreads, OWN ? own_waves(DT, PACKED) : many_waves(
         }
       }
       float top = __builtin_amdgcn_exp2f(mx - m) * vs_top;
-      if (!rows_all(most >= 0.25f * top)) top = max_of_groups(most);
+      const uint32_t near = rows_with(most >= 0.25f * top);
+      if (near != 0xFFFFu) {
+        most = max_of_groups(most);
+        top = near >> lr & 1u ? top : most;   // a row's own affair, whatever the others do
+      }
       top = fmaxf(top, 0x1p-100f);
       const float to = kDigits * __builtin_amdgcn_rcpf(top);
       unit = top * (1.0f / kDigits) * (PACKED ? 0.0625f : 1.0f);

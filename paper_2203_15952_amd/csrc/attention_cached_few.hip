@@ -190,7 +190,7 @@ __global__ __launch_bounds__(kThreads, few_waves(DT, PACKED, R)) void attention_
     vs = any ? vs : 0.0f;
     const float vs_top = wave_max_positive(vs);
     float alpha[R], unit[R], weight[R], top[R];
-    bool near = true;
+    bool near[R], all_near = true;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       const float mx = wave_max_signed(see[r] ? s[r] : kLowest), mnew = fmaxf(m[r], mx);
@@ -200,11 +200,13 @@ __global__ __launch_bounds__(kThreads, few_waves(DT, PACKED, R)) void attention_
       l[r] = fmaf(l[r], alpha[r], p);
       weight[r] = p * vs;
       top[r] = __builtin_amdgcn_exp2f(mx - mnew) * vs_top;
-      near = near && __any(weight[r] >= 0.25f * top[r]);
+      near[r] = __any(weight[r] >= 0.25f * top[r]);
+      all_near = all_near && near[r];
     }
-    if (!near) {
+    if (!all_near) {
 #pragma unroll
-      for (int r = 0; r < R; ++r) top[r] = wave_max_positive(weight[r]);
+      for (int r = 0; r < R; ++r)
+        if (!near[r]) top[r] = wave_max_positive(weight[r]);
     }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
