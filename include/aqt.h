@@ -683,7 +683,8 @@ size_t aqt_cache_bytes(const aqt_cache *shape);
  * Write the keys and values of T new frames per stream, qkv [streams * T, (heads + 2 kv_heads) dh]
  * (rows as above), into the cache: stream b's frame length[b] + t takes the place of the one
  * `capacity` frames before it (of a call longer than the capacity only the last frames stay).
- * *dev_status is set to AQT_ERR_NONFINITE when a head's abs-max is Inf/NaN.
+ * *dev_status is set to AQT_ERR_NONFINITE when a head's abs-max is Inf/NaN; that key or value is kept as
+ * NaN: it reads back as NaN in all its columns, and every row of the attention that sees it is NaN.
  */
 aqt_status aqt_cache_append(const float *qkv, int64_t T, int heads, const aqt_cache *cache, const int32_t *count,
                             void *stream, int32_t *dev_status);
@@ -709,7 +710,8 @@ aqt_status aqt_cache_advance(int64_t *length, int64_t streams, int64_t T, const 
  * heads / kv_heads share key / value head h / (heads / kv_heads).  ctx [streams * T, heads dh]: rows
  * of frames that a stream does not bring stay as they are; a row that sees no frame (its window lies
  * before what the cache still holds) is zeros.  ctx_absmax nullable device float: max|ctx| over the
- * written rows, cleared by the call.  A non-finite query gives NaN in its row.
+ * written rows, cleared by the call.  A non-finite query gives NaN in its row, a key or value kept as NaN
+ * in the rows that see its frame; rows that do not see it come out as if it were not there.
  * Needs aqt_attention_cached_workspace_bytes() (it does not depend on lengths or windows).
  */
 size_t aqt_attention_cached_workspace_bytes(const aqt_cache *cache, int64_t T, int heads);

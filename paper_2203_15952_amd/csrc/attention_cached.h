@@ -72,6 +72,9 @@ __device__ __forceinline__ uint32_t rows_with(bool has) {
   return static_cast<uint32_t>(b | b >> 16) & 0xFFFFu;
 }
 
+// Of a number that is not negative; a NaN stays one.
+__device__ __forceinline__ float at_least_tiny(float v) { return __uint_as_float(max(__float_as_uint(v), 0x0D800000u)); }   // 2^-100
+
 // The largest of a wavefront's 64 words.  (The steps fuse with the moves between lanes, as they do not for float32.)
 __device__ __forceinline__ uint32_t wave_max(uint32_t v) {
   auto step = [&](int w) { v = max(v, static_cast<uint32_t>(w)); };

@@ -243,11 +243,19 @@ __global__ __launch_bounds__(kThreads, OWN ? own_waves(DT, PACKED) : many_waves(
       }
       float top = __builtin_amdgcn_exp2f(mx - m) * vs_top;
       const uint32_t near = rows_with(most >= 0.25f * top);
-      if (near != 0xFFFFu) {
-        most = max_of_groups(most);
-        top = near >> lr & 1u ? top : most;   // a row's own affair, whatever the others do
+      if (near != 0xFFFFu) {   // ... and where a scale is NaN: what a row does not see is nothing to it
+        uint32_t own = 0u;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int j = j0 + 16 * (e >> 2) + 4 * lg + (e & 3);
+          s[e] = j >= lo && j <= hi ? s[e] : 0.0f;
+          own = max(own, __float_as_uint(s[e]) & 0x7FFFFFFFu);
+        }
+        own = max(own, static_cast<uint32_t>(__shfl_xor(static_cast<int>(own), 16, 64)));
+        own = max(own, static_cast<uint32_t>(__shfl_xor(static_cast<int>(own), 32, 64)));
+        top = near >> lr & 1u ? top : __uint_as_float(own);   // a row's own affair, whatever the others do
       }
-      top = fmaxf(top, 0x1p-100f);
+      top = at_least_tiny(top);
       const float to = kDigits * __builtin_amdgcn_rcpf(top);
       unit = top * (1.0f / kDigits) * (PACKED ? 0.0625f : 1.0f);
 #pragma unroll

@@ -203,14 +203,16 @@ __global__ __launch_bounds__(kThreads, few_waves(DT, PACKED, R)) void attention_
       near[r] = __any(weight[r] >= 0.25f * top[r]);
       all_near = all_near && near[r];
     }
-    if (!all_near) {
+    if (!all_near) {   // ... and where a scale is NaN: what a row does not see is nothing to it
 #pragma unroll
-      for (int r = 0; r < R; ++r)
-        if (!near[r]) top[r] = wave_max_positive(weight[r]);
+      for (int r = 0; r < R; ++r) {
+        weight[r] = see[r] ? weight[r] : 0.0f;
+        if (!near[r]) top[r] = wave_max_positive(fabsf(weight[r]));
+      }
     }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      top[r] = fmaxf(top[r], 0x1p-100f);
+      top[r] = at_least_tiny(top[r]);
       unit[r] = top[r] * (1.0f / kDigits) * (PACKED ? 0.0625f : 1.0f);
       const uint32_t u = weight_bits(weight[r], kDigits * __builtin_amdgcn_rcpf(top[r])) ^ 0x00008080u;
       put[(2 * R + r) * 64] = static_cast<uint8_t>(u);

@@ -148,7 +148,8 @@ __global__ __launch_bounds__(kThreads) void cache_append_kernel(const float *__r
   }
   const bool odd = j & 1, upper = j & 2, own = upper ? (odd ? mine[3] : mine[2]) : odd ? mine[1] : mine[0];
   const uint32_t own_top = upper ? (odd ? top[3] : top[2]) : odd ? top[1] : top[0];
-  const float fq = static_cast<float>(g.qmax), own_s = __uint_as_float(own_top) / fq;
+  // (Inf or NaN in the head: a scale of NaN, which makes NaN of all that is read from it, whatever the codes are)
+  const float fq = static_cast<float>(g.qmax), own_s = own_top < 0x7F800000u ? __uint_as_float(own_top) / fq : __builtin_nanf("");
   const float own_r = own_s > 0x1p-60f && own_s < 0x1p60f ? __builtin_amdgcn_rcpf(own_s) : 0.0f;
   if (j < 4 && own) {
     reinterpret_cast<float *>(tile + cache_scales(g))[(q.values ? 64 : 0) + key + j] = own_s;

@@ -168,11 +168,60 @@ static void weights() {
   drawn_sizes(2, 1, 64, 8);
   drawn_sizes(5, 2, 64, 4);
 }
+// A number that is none in the key or the value of a frame: NaN in all rows that see it and read back, nothing in the others.
+static void one_nonfinite(int T, int group, int dh, int bits, int at, int64_t left, int64_t right, float what, bool key) {
+  printf("%f in the %s of frame %d: %d new, group %d, dh %d, bits %d\n", what, key ? "key" : "value", at, T, group, dh, bits); fflush(stdout);
+  Rows r = make_rows(130, T, group, dh, bits);
+  for (int h = 0; h < group; ++h) r.query(r.frames - T, h)[dh / 2] = -1.0f;   // (an infinite key against a query of either sign)
+  float *const row = key ? r.key(at) : r.value(at);
+  row[dh / 2] = what;
+  Cached c;
+  fill(c, r);
+  for (int form = 0; form < 5; ++form) {
+    const std::vector<float> got = attend_form(c, r, left, right, form);
+    if (got.empty()) continue;
+    for (int t = 0; t < T; ++t) for (int h = 0; h < group; ++h) {
+      const int64_t f = r.frames - T + t;
+      const bool seen = (left < 0 || at >= f - left) && (right < 0 || at <= f + right);
+      const Want w = want_of(c, r, t, h, left, right);
+      for (int e = 0; e < dh; ++e) {
+        const float x = got[((size_t)t * group + h) * dh + e];
+        if (seen ? !std::isnan(x) : !(fabs((double)x - w.o[e]) <= w.tol * w.mag)) {
+          printf("  form %d row %d head %d column %d: %g, seen %d\n", form, t, h, e, x, seen);
+          complain("a number that is none");
+          t = T; h = group;
+          break;
+        }
+      }
+    }
+  }
+  const int L = cache_::lanes_of(dh), per = (int)cache_::cut_of(c.g, r.frames).blocks, run_ = cache_::cut_of(c.g, r.frames).log2_run;
+  const bool vec = dh % 4 == 0;
+  std::vector<float> keys((size_t)r.frames * dh, 7.0f), values((size_t)r.frames * dh, 7.0f);
+  auto rd = L == 4 ? (vec ? read_<4, true> : read_<4, false>) : L == 8 ? (vec ? read_<8, true> : read_<8, false>) : (vec ? read_<16, true> : read_<16, false>);
+  rd((unsigned)per, c.g, T, nullptr, nullptr, r.frames, run_, per, keys.data(), values.data());
+  for (int j = 0; j < r.frames; ++j) for (int e = 0; e < dh; ++e) {
+    const size_t i = (size_t)j * dh + e;
+    if (std::isnan(keys[i]) != (key && j == at) || std::isnan(values[i]) != (!key && j == at)) { complain("read back"); j = r.frames; break; }
+  }
+  free(c.g.data);
+}
+static void nonfinite() {
+  for (float what : {NAN, INFINITY, -INFINITY}) for (bool key : {false, true}) {
+    one_nonfinite(4, 1, 64, 8, 127, -1, 0, what, key);    // seen by the last three of four
+    one_nonfinite(12, 1, 36, 4, 125, -1, 0, what, key);   // ... by five of twelve
+    one_nonfinite(9, 3, 128, 8, 61, 64, 1, what, key);    // ... by the first five of nine, in another tile than theirs
+  }
+  one_nonfinite(1, 2, 20, 8, 3, -1, 0, NAN, false);
+  one_nonfinite(2, 1, 64, 4, 129, -1, 0, NAN, false);
+  one_nonfinite(20, 1, 128, 4, 129, 40, 0, NAN, false);
+}
 }  // namespace aqt
 int main(int argc, char **argv) {
   using namespace aqt;
   const std::string what = argc > 1 ? argv[1] : "";
   if (what == "weights") weights();
+  else if (what == "nonfinite") nonfinite();
   else complain("no such test");
   printf(bad ? "MISMATCH\n" : "ok\n");
   return bad;

@@ -106,3 +106,41 @@ def test_values_of_all_sizes(form, window):
         q *= F(3)
         v *= np.exp2(rng.uniform(-20, 0, v.shape[:2])).astype(F)[:, :, None, None]
     compare(form, change, *window)
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("bad", [np.nan, np.inf, -np.inf])
+@pytest.mark.parametrize("in_key", [False, True])
+def test_numbers_that_are_none(form, bad, in_key):
+    """In one column of one frame's key or value: the head reads back as NaN, and the rows that see the frame are NaN in every column;
+    the others come out as if it were not there.  The frame: one from the middle of the call's, which half of its rows see."""
+    streams, capacity, heads, kv, dh, bits, n, T = form
+    say("none", form, bad, in_key)
+    rng = np.random.default_rng(n + T + dh)
+    rows = rng.standard_normal((streams, n, heads + 2 * kv, dh)).astype(F)
+    at, head = n - 1 - T // 2, kv - 1
+    clean = rows.copy()
+    rows[-1, at, heads + head + (0 if in_key else kv), dh // 2] = bad
+    cache, ref = make(streams, capacity, heads, kv, dh, bits)
+    for lo, hi in ((0, n - T), (n - T, n)):
+        if hi > lo:
+            status = B.new_status()
+            new = dev(np.ascontiguousarray(rows[:, lo:hi]).reshape(-1, ref.cols))
+            B.aqt_cache_append(new, cache, hi - lo, heads, dev_status=status)
+            assert host(status)[0] == (B.AQT_ERR_NONFINITE if lo <= at < hi else 0)
+            ref.append(np.ascontiguousarray(clean[:, lo:hi]).reshape(-1, ref.cols), hi - lo)
+            if hi < n:
+                cache.advance(hi - lo)
+    got, m = B.aqt_attention_cached_fwd(new, cache, T, heads, left=T, right=0, want_absmax=True)
+    want, tol = expected(ref, clean[:, n - T:].reshape(-1, ref.cols), T, T, 0)
+    got, want, tol = (a.reshape(streams, T, kv, heads // kv, dh) for a in (host(got), want, tol))
+    sees = np.arange(n - T, n) >= at
+    assert sees.any() and np.isnan(got[-1, sees, head]).all() and np.isnan(float(m))
+    keep = np.ones(got.shape, bool)
+    keep[-1, sees, head] = False
+    assert (np.abs(got - want) <= tol + 1e-30)[keep].all()
+    keys, values = (host(t).reshape(streams, n, kv, dh) for t in B.aqt_cache_read(cache, n, pending=T))
+    hit = np.zeros(keys.shape, bool)
+    hit[-1, at, head] = True
+    np.testing.assert_array_equal(np.isnan(keys), hit & in_key)
+    np.testing.assert_array_equal(np.isnan(values), hit & (not in_key))
