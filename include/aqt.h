@@ -692,8 +692,9 @@ aqt_status aqt_cache_append(const float *qkv, int64_t T, int heads, const aqt_ca
 /*
  * Read n frames per stream back as code * scale: keys and / or values (either may be NULL)
  * [streams * n, kv_heads dh], row (b, i) from frame first[b] + i; first NULL: the last n.
- * The stream has length[b] + (count ? count[b] : pending) frames then: pending / count name what was
- * appended and not advanced over yet (pending >= 0; 0 with count NULL: the length as it stands).
+ * pending and count name what was appended and not advanced over yet, as the append's T and count did:
+ * the stream has length[b] + pending frames then, or with count as many of them as it brought (outside
+ * 0..pending: the nearest).  pending 0: the length as it stands; count without pending is refused.
  * Frames that it does not have, or the cache no longer holds, read as zeros.
  */
 aqt_status aqt_cache_read(const aqt_cache *cache, int64_t pending, const int32_t *count, const int64_t *first,

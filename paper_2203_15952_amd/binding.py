@@ -1024,7 +1024,8 @@ def aqt_cache_append(qkv, cache: KvCache, T: int, heads: int, *, count=None, dev
 def aqt_cache_read(cache: KvCache, n: int, *, first=None, pending: int = 0, count=None, keys=None, values=None, want_keys=True,
                    want_values=True):
     """aqt_cache_read: returns (keys, values) float32 [streams*n, kv_heads dh], the frames first[b] .. (int64 [streams]; default
-    the last n).  pending / count: appended frames that cache.length does not count yet."""
+    the last n).  pending: frames per stream of an append that cache.length does not count yet (its T); count: how many of them
+    each stream brought (its count; only with pending)."""
     dev = _current(cache.data, "cache")
     shape = (cache.streams * n, cache.kv_heads * cache.dh)
     if first is not None:

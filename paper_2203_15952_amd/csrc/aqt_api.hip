@@ -1150,7 +1150,7 @@ aqt_status aqt_cache_append(const float *qkv, int64_t T, int heads, const aqt_ca
 aqt_status aqt_cache_read(const aqt_cache *cache, int64_t pending, const int32_t *count, const int64_t *first, int64_t n, float *keys,
                           float *values, void *stream) {
   AQT_TRY(cache_check(cache));
-  if (!cache_buffers_ok(*cache) || pending < 0 || n < 1 || (!keys && !values)) return AQT_ERR_INVALID_ARG;
+  if (!cache_buffers_ok(*cache) || pending < 0 || (count && pending < 1) || n < 1 || (!keys && !values)) return AQT_ERR_INVALID_ARG;
   if (n > (int64_t(1) << 40) || pending > (int64_t(1) << 40)) return AQT_ERR_UNSUPPORTED;
   return launch_cache_read(*cache, pending, count, first, n, keys, values, static_cast<hipStream_t>(stream));
 }
