@@ -200,7 +200,7 @@ __global__ __launch_bounds__(kThreads, OWN ? own_waves(DT, PACKED) : many_waves(
         }
         const v4f ks = *reinterpret_cast<const v4f *>(&sc[16 * t + 4 * lg]);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) s[4 * t + r] = joined(c[0][r], c[1][r], c[2][r]) * ks[r] * row_scale;
+        for (int r = 0; r < 4; ++r) s[4 * t + r] = joined(c[0][r], c[1][r], c[2][r]) * (ks[r] * row_scale);   // (the sum, up to 2^37, by the small factor)
       }
       load_keys(next);
       if (!whole) {   // what the window hides, and what is no frame of the stream's, may hold anything

@@ -216,12 +216,31 @@ static void nonfinite() {
   one_nonfinite(2, 1, 64, 4, 129, -1, 0, NAN, false);
   one_nonfinite(20, 1, 128, 4, 129, 40, 0, NAN, false);
 }
+// Small queries against large keys, and the other way round: scores of ordinary size.
+static void scores_of(int T, int group, int dh, int bits, float q, float k) {
+  Rows r = make_rows(130, T, group, dh, bits);
+  for (int j = 0; j < r.frames; ++j) for (int e = 0; e < dh; ++e) {
+    for (int h = 0; h < group; ++h) r.query(j, h)[e] *= q;
+    r.key(j)[e] *= k;
+  }
+  char what[64];
+  snprintf(what, sizeof what, "queries x %g, keys x %g", q, k);
+  compare(r, -1, 0, what);
+}
+static void scores() {
+  for (auto [q, k] : {std::pair<float, float>{1e-30f, 1e30f}, {1e-28f, 1e27f}, {1e30f, 1e-30f}, {3e-30f, 1e36f / 4e6f}}) {
+    scores_of(2, 1, 64, 8, q, k);
+    scores_of(9, 2, 128, 4, q, k);
+    scores_of(20, 1, 128, 8, q, k);
+  }
+}
 }  // namespace aqt
 int main(int argc, char **argv) {
   using namespace aqt;
   const std::string what = argc > 1 ? argv[1] : "";
   if (what == "weights") weights();
   else if (what == "nonfinite") nonfinite();
+  else if (what == "scores") scores();
   else complain("no such test");
   printf(bad ? "MISMATCH\n" : "ok\n");
   return bad;

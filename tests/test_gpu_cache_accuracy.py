@@ -144,3 +144,14 @@ def test_numbers_that_are_none(form, bad, in_key):
     hit[-1, at, head] = True
     np.testing.assert_array_equal(np.isnan(keys), hit & in_key)
     np.testing.assert_array_equal(np.isnan(values), hit & (not in_key))
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("qs,ks", [(1e-30, 1e30), (1e30, 1e-30), (1e-28, 1e28)])
+def test_scores_of_ordinary_size_from_small_and_large_factors(form, qs, ks):
+    say("factors", form, qs, ks)
+
+    def change(q, k, v):
+        q *= F(qs)
+        k *= F(ks)
+    compare(form, change)
