@@ -39,6 +39,42 @@ __device__ __forceinline__ void digits4(const int (&n)[4], int &d0, int &d1, int
   d0 = static_cast<int>(__builtin_amdgcn_perm(ct, at, 0x05040100u));
 }
 
+// Whether a lane's 16 KS columns x of a row (from column 16 lg and 64 + 16 lg on, zeros behind dh) say that the row, whose largest column
+// is `top`, loses by integers relative to that: eight of them (twelve of 32, all others in narrow heads) lie under 1 / 64 of it.
+// One in 25 of normally distributed columns does: it takes a row of 64 such columns once in three million (with six of them once in
+// ten thousand: one call in two of 8192 rows over a long history then waited for a row that it had taken, 62 us for 50).
+template <int KS>
+__device__ __forceinline__ bool lane_is_wide(const float (&x)[KS][16], float top, int lg, int dh) {
+  const float below = top * 0.015625f;
+  int small = 0;
+#pragma unroll
+  for (int k = 0; k < KS; ++k) {
+    small -= min(max(64 * k + 16 * lg + 16 - dh, 0), 16);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) small += fabsf(x[k][i]) < below ? 1 : 0;
+  }
+  return small >= min(max(dh - 1, 1), KS == 1 ? 8 : 12) && top < __builtin_inff();
+}
+// What a row's integers x `to` leave of it, in units of 2^-23 of theirs and again as digits (nothing of rows that are not wide: their
+// scores are the same with and without).
+__device__ __forceinline__ void rest_digits(const float (&x)[16], float to, bool wide, v4i (&d)[3]) {
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    int n[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float v = x[4 * w + i];
+      n[i] = wide ? static_cast<int>(rintf(fmaf(v, to, -rintf(v * to)) * 8388608.0f)) : 0;
+    }
+    int d0, d1, d2;
+    digits4(n, d0, d1, d2);
+    d[0][w] = d0;
+    d[1][w] = d1;
+    d[2][w] = d2;
+  }
+}
+constexpr float kRestUnit = 1.0f / 8388608.0f;
+
 // A weight of 0 .. 1 as an integer w of 23 bits: 0x808080 + w, as a float of the binade 2^23 .. 2^24, whose steps are ones; the
 // sum rounds to nearest.  Its bytes are the balanced digits (the highest lacks the sign bit that the exponent's place took; the others
 // are off by 128, i.e. by their highest bit).

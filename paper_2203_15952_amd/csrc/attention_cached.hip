@@ -2,10 +2,16 @@
 //   score_j = (q . codes_j) s_j / sqrt(dh),   p = softmax over the frames j that the window admits and the cache holds,
 //   ctx = sum_j p_j s'_j codes'_j          (s, s' the scales of the frame's key and value).
 // The codes never become floats: both products run on the int8 matrix cores (v_mfma_i32_16x16x64_i8, exact 32-bit sums), and it
-// is the float operand that is carried whole, as an integer of 24 bits relative to its row's largest, in three balanced
-// base-256 digits, i.e. three int8 operands.  (A code turned into bf16 costs a vector instruction or two for every code of
-// the cache; the digits of a query are made once, those of a probability once for all columns of the values.)  An integer
-// rounded at 2^-24 of the largest is as good as a float32 sum over the row.
+// is the float operand that becomes an integer of 24 bits, in three balanced base-256 digits, i.e. three int8 operands.  (A code
+// turned into bf16 costs a vector instruction or two for every code of the cache; the digits of a query are made once, those of a
+// weight once for all columns of the values.)
+// What is rounded, and to what: a query's columns to 2^-24 of the row's largest column, as good as a float32 sum where that is like
+// the others.  Where a column stands out of its row it may meet keys of zero, and would leave the others the bits that it has not
+// taken (r times their size, r = 64, 1000, 10^6: errors of the result of 2e-6, 4e-5, 4e-2): the integers of such rows (lane_is_wide)
+// are followed by 23 bits more, whose products a branch that all other tiles step over adds to the scores.  A frame's weight p_j s'_j
+// is rounded to 2^-24 .. 2^-22 of the largest of its tile: relative to sum_j p_j max|v_j| a float32 sum's error or less, but not
+// column by column: where the frame with the weight has a value of zero in a column, and a large one in another, the other frames'
+// values in that column keep the bits that are left.  (Codes are off by 2^-8 and more of a value's largest column anyway.)
 //
 // A workgroup owns 16 rows (frame, query head) that share a key / value head, and its wavefronts take the tiles of 64 frames
 // in turn, each with its own running maximum and sum, joined through LDS at the end; where that leaves the chip empty, several
@@ -59,6 +65,7 @@ __global__ __launch_bounds__(kThreads, OWN ? own_waves(DT, PACKED) : many_waves(
   using P = Partial<kRows, COLS>;
   __shared__ __attribute__((aligned(16))) float so[kWaves][kRows][LD];
   __shared__ __attribute__((aligned(16))) float scales[kWaves][128];
+  __shared__ __attribute__((aligned(16))) int rest[kWaves][KS][3][64][4];   // of rows whose integers do not hold them
   __shared__ float sm[kWaves][kRows], sl[kWaves][kRows];
   const int tid = static_cast<int>(threadIdx.x), lane = tid & 63, lr = lane & 15, lg = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -98,14 +105,15 @@ __global__ __launch_bounds__(kThreads, OWN ? own_waves(DT, PACKED) : many_waves(
   key_piece keys[4][KS];
   v4i values[VALUES];
   float ks_next, vs_next;
+  auto key_of = [&](const uint8_t *tile, int t, int k) {   // sixteen columns to a lane; one beyond the row meets digits of zero
+    const int at = (64 * k + 16 * lg) * KEYS / 4;
+    return *reinterpret_cast<const key_piece *>(tile + (16 * t + lr) * g.key_row + (at < g.key_row ? at : 0));
+  };
   auto load_keys = [&](const uint8_t *tile) {
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
-      for (int k = 0; k < KS; ++k) {   // sixteen columns to a lane; one beyond the row meets digits of zero
-        const int at = (64 * k + 16 * lg) * KEYS / 4;
-        keys[t][k] = *reinterpret_cast<const key_piece *>(tile + (16 * t + lr) * g.key_row + (at < g.key_row ? at : 0));
-      }
+      for (int k = 0; k < KS; ++k) keys[t][k] = key_of(tile, t, k);
     ks_next = reinterpret_cast<const float *>(tile + cache_scales(g))[lane];
     vs_next = reinterpret_cast<const float *>(tile + cache_scales(g))[64 + lane];
   };
@@ -133,6 +141,7 @@ __global__ __launch_bounds__(kThreads, OWN ? own_waves(DT, PACKED) : many_waves(
   // their digits
   v4i q[KS][3];
   float row_scale;
+  bool wide;
   {
     uint32_t m = 0u;
 #pragma unroll
@@ -160,9 +169,31 @@ __global__ __launch_bounds__(kThreads, OWN ? own_waves(DT, PACKED) : many_waves(
         q[k][1][w] = d1;
         q[k][2][w] = d2;
       }
+    const uint32_t wide_rows = rows_with(lane_is_wide<KS>(x, top, lg, g.dh));
+    wide = wide_rows != 0u;
+    if (wide) {
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {
+        v4i d[3];
+        rest_digits(x[k], to, wide_rows >> lr & 1u, d);
+#pragma unroll
+        for (int e = 0; e < 3; ++e) *reinterpret_cast<v4i *>(rest[wave][k][e][lane]) = d[e];
+      }
+      wave_lds_order();
+    }
   }
+  auto codes = [&](key_piece x) {
+    if constexpr (PACKED) {
+      const uint32_t lo8 = static_cast<uint32_t>(x[0]), hi8 = static_cast<uint32_t>(x[1]);
+      return v4i{static_cast<int>(lo8 << 4 & 0xF0F0F0F0u), static_cast<int>(hi8 << 4 & 0xF0F0F0F0u), static_cast<int>(lo8 & 0xF0F0F0F0u),
+                 static_cast<int>(hi8 & 0xF0F0F0F0u)};
+    } else {
+      return x;
+    }
+  };
 
   for (; i < tiles; i += step) {
+    const uint8_t *const tile = head + static_cast<int64_t>(slot) * g.tile_bytes;
     if (i + step < tiles) {   // otherwise this tile's once more: never another's memory
       slot += slot_step;
       slot = slot >= g.tiles ? slot - g.tiles : slot;
@@ -187,14 +218,7 @@ __global__ __launch_bounds__(kThreads, OWN ? own_waves(DT, PACKED) : many_waves(
         v4i c[3];
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
-          v4i w;
-          if constexpr (PACKED) {
-            const uint32_t x = static_cast<uint32_t>(keys[t][k][0]), y = static_cast<uint32_t>(keys[t][k][1]);
-            w = v4i{static_cast<int>(x << 4 & 0xF0F0F0F0u), static_cast<int>(y << 4 & 0xF0F0F0F0u), static_cast<int>(x & 0xF0F0F0F0u),
-                    static_cast<int>(y & 0xF0F0F0F0u)};
-          } else {
-            w = keys[t][k];
-          }
+          const v4i w = codes(keys[t][k]);
 #pragma unroll
           for (int d = 0; d < 3; ++d) c[d] = mfma_i8(w, q[k][d], k == 0 ? v4i{0, 0, 0, 0} : c[d]);
         }
@@ -203,6 +227,24 @@ __global__ __launch_bounds__(kThreads, OWN ? own_waves(DT, PACKED) : many_waves(
         for (int r = 0; r < 4; ++r) s[4 * t + r] = joined(c[0][r], c[1][r], c[2][r]) * (ks[r] * row_scale);   // (the sum, up to 2^37, by the small factor)
       }
       load_keys(next);
+      if (wide) {   // the digits behind those (few rows have any, so that the tile's keys are read again)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          v4f sum = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+          for (int d = 0; d < 3; ++d) {
+            v4i c = {0, 0, 0, 0};
+#pragma unroll
+            for (int k = 0; k < KS; ++k) c = mfma_i8(codes(key_of(tile, t, k)), *reinterpret_cast<const v4i *>(rest[wave][k][d][lane]), c);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) sum[r] = fmaf(sum[r], 256.0f, static_cast<float>(c[r]));
+          }
+          const v4f ks = *reinterpret_cast<const v4f *>(&sc[16 * t + 4 * lg]);
+#pragma unroll
+          for (int r = 0; r < 4; ++r) s[4 * t + r] = fmaf(sum[r], ks[r] * row_scale * kRestUnit, s[4 * t + r]);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
       if (!whole) {   // what the window hides, and what is no frame of the stream's, may hold anything
         asm volatile("");   // a branch: as selections they would be taken in every tile
 #pragma unroll

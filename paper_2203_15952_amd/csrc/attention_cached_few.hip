@@ -32,6 +32,7 @@ __global__ __launch_bounds__(kThreads, few_waves(DT, PACKED, R)) void attention_
   constexpr int KS = DT == 8 ? 2 : 1, COLS = 16 * DT, HALVES = DT == 8 ? 2 : 1, BLOCKS = DT < 4 ? DT : 4;   // HALVES of 64 columns
   using P = Partial<R, COLS>;
   __shared__ __attribute__((aligned(16))) uint8_t digits[kWaves][3][R][64];
+  __shared__ __attribute__((aligned(16))) int rest[kWaves][KS][3][64][4];   // of rows whose integers do not hold them
   __shared__ float so[kWaves][R][COLS], sm[kWaves][R], sl[kWaves][R];
   const int tid = static_cast<int>(threadIdx.x), lane = tid & 63, lr = lane & 15, lg = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -87,14 +88,15 @@ __global__ __launch_bounds__(kThreads, few_waves(DT, PACKED, R)) void attention_
   key_piece keys[4][KS];
   v4i values[VALUES];
   float ks, vs_next;
+  auto key_of = [&](const uint8_t *tile, int t, int k) {   // sixteen columns to a lane; one beyond the row meets digits of zero
+    const int at = (64 * k + 16 * lg) * KEYS / 4;
+    return *reinterpret_cast<const key_piece *>(tile + (16 * t + lr) * g.key_row + (at < g.key_row ? at : 0));
+  };
   auto load_keys = [&](const uint8_t *tile) {
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
-      for (int k = 0; k < KS; ++k) {   // sixteen columns to a lane; one beyond the row meets digits of zero
-        const int at = (64 * k + 16 * lg) * KEYS / 4;
-        keys[t][k] = *reinterpret_cast<const key_piece *>(tile + (16 * t + lr) * g.key_row + (at < g.key_row ? at : 0));
-      }
+      for (int k = 0; k < KS; ++k) keys[t][k] = key_of(tile, t, k);
     ks = reinterpret_cast<const float *>(tile + cache_scales(g))[lane];
   };
   auto load_values = [&](const uint8_t *tile) {
@@ -115,6 +117,7 @@ __global__ __launch_bounds__(kThreads, few_waves(DT, PACKED, R)) void attention_
   // the rows' digits: row lr % 4 of R, 16 columns per lane and step
   v4i q[KS][3];
   float row_scale[R];
+  bool wide;
   {
     uint32_t m = 0u;
 #pragma unroll
@@ -144,9 +147,31 @@ __global__ __launch_bounds__(kThreads, few_waves(DT, PACKED, R)) void attention_
         q[k][1][w] = d1;
         q[k][2][w] = d2;
       }
+    const uint32_t wide_rows = rows_with(lane_is_wide<KS>(x, top, lg, g.dh));
+    wide = wide_rows != 0u;
+    if (wide) {
+#pragma unroll
+      for (int k = 0; k < KS; ++k) {
+        v4i d[3];
+        rest_digits(x[k], to, wide_rows >> lr & 1u, d);
+#pragma unroll
+        for (int e = 0; e < 3; ++e) *reinterpret_cast<v4i *>(rest[wave][k][e][lane]) = d[e];
+      }
+      wave_lds_order();
+    }
   }
+  auto codes = [&](key_piece x) {
+    if constexpr (PACKED) {
+      const uint32_t lo8 = static_cast<uint32_t>(x[0]), hi8 = static_cast<uint32_t>(x[1]);
+      return v4i{static_cast<int>(lo8 << 4 & 0xF0F0F0F0u), static_cast<int>(hi8 << 4 & 0xF0F0F0F0u), static_cast<int>(lo8 & 0xF0F0F0F0u),
+                 static_cast<int>(hi8 & 0xF0F0F0F0u)};
+    } else {
+      return x;
+    }
+  };
 
   for (; i < tiles; i += step) {
+    const uint8_t *const tile = head + static_cast<int64_t>(slot) * g.tile_bytes;
     if (i + step < tiles) {   // otherwise this tile's once more: never another's memory
       slot += slot_step;
       slot = slot >= g.tiles ? slot - g.tiles : slot;
@@ -159,14 +184,7 @@ __global__ __launch_bounds__(kThreads, few_waves(DT, PACKED, R)) void attention_
     for (int t = 0; t < 4; ++t)
 #pragma unroll
       for (int k = 0; k < KS; ++k) {
-        v4i w;
-        if constexpr (PACKED) {
-          const uint32_t x = static_cast<uint32_t>(keys[t][k][0]), y = static_cast<uint32_t>(keys[t][k][1]);
-          w = v4i{static_cast<int>(x << 4 & 0xF0F0F0F0u), static_cast<int>(y << 4 & 0xF0F0F0F0u), static_cast<int>(x & 0xF0F0F0F0u),
-                  static_cast<int>(y & 0xF0F0F0F0u)};
-        } else {
-          w = keys[t][k];
-        }
+        const v4i w = codes(keys[t][k]);
 #pragma unroll
         for (int d = 0; d < 3; ++d) c[t][d] = mfma_i8(q[k][d], w, k == 0 ? v4i{0, 0, 0, 0} : c[t][d]);
       }
@@ -186,6 +204,24 @@ __global__ __launch_bounds__(kThreads, few_waves(DT, PACKED, R)) void attention_
       see[r] = whole || (j >= lo[r] && j <= hi[r]);
       any = any || see[r];
       s[r] = joined(d[0], d[1], d[2]) * (row_scale[r] * ks_now);
+    }
+    if (wide) {   // the digits behind those (few rows have any, so that the tile's keys are read again)
+      float sum[R];
+#pragma unroll
+      for (int r = 0; r < R; ++r) sum[r] = 0.0f;
+#pragma unroll
+      for (int d = 0; d < 3; ++d) {
+        v4i e[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int k = 0; k < KS; ++k)
+            e[t] = mfma_i8(*reinterpret_cast<const v4i *>(rest[wave][k][d][lane]), codes(key_of(tile, t, k)), k == 0 ? v4i{0, 0, 0, 0} : e[t]);
+#pragma unroll
+        for (int r = 0; r < R; ++r) sum[r] = fmaf(sum[r], 256.0f, static_cast<float>(of_group(e[0][r], e[1][r], e[2][r], e[3][r], odd, upper)));
+      }
+#pragma unroll
+      for (int r = 0; r < R; ++r) s[r] = fmaf(sum[r], row_scale[r] * ks_now * kRestUnit, s[r]);
     }
     vs = any ? vs : 0.0f;
     const float vs_top = wave_max_positive(vs);

@@ -73,15 +73,18 @@ static std::vector<float> attend_form(Cached &c, Rows &r, int64_t left, int64_t 
 // are off by half a unit of its largest column over 2^23, and eight roundings.  A weight: an integer of which the largest of a tile is
 // 2^21 at least, so half a unit is 4 U of it, for each of 64 frames; four roundings for every tile, the sum of weights sixteen.
 struct Want { std::vector<double> o; double mag, tol; };
-static Want want_of(const Cached &c, Rows &r, int t, int h, int64_t left, int64_t right) {
+// wide: a row of which a column stands out far.  Then the query's digits go on for 23 bits, and what is left is the rounding of their sums:
+// 2^-24 of the magnitudes of the products.
+static Want want_of(const Cached &c, Rows &r, int t, int h, int64_t left, int64_t right, bool wide = false) {
   const int64_t f = r.frames - r.T + t, lo = left < 0 ? 0 : std::max<int64_t>(0, f - left), hi = right < 0 ? r.frames - 1 : std::min<int64_t>(r.frames - 1, f + right);
   const float *q = r.query((int)f, h);
-  double qmax = 0, top = -1e300, reach = 0, largest = 0, spread = 0, sum = 0;
+  double qmax = 0, top = -1e300, reach = 0, terms = 0, largest = 0, spread = 0, sum = 0;
   for (int e = 0; e < r.dh; ++e) qmax = std::max(qmax, (double)fabsf(q[e]));
   std::vector<double> s;
   for (int64_t j = lo; j <= hi; ++j) {
-    double d = 0, m = 0;
-    for (int e = 0; e < r.dh; ++e) { d += c.k[j][e] * q[e]; m += fabs(c.k[j][e]); }
+    double d = 0, m = 0, a = 0;
+    for (int e = 0; e < r.dh; ++e) { d += c.k[j][e] * q[e]; m += fabs(c.k[j][e]); a += fabs(c.k[j][e] * q[e]); }
+    terms = std::max(terms, a / sqrt((double)r.dh));
     s.push_back(d / sqrt((double)r.dh));
     top = std::max(top, s.back()); largest = std::max(largest, fabs(s.back())); reach = std::max(reach, qmax * m / sqrt((double)r.dh));
   }
@@ -94,12 +97,12 @@ static Want want_of(const Cached &c, Rows &r, int t, int h, int64_t left, int64_
     w.mag += p * most;
   }
   // (frames whose score lies more than 110 below the largest weigh nothing, and their roundings neither)
-  const double e = kU * reach + 8 * kU * largest + kU * (std::min(spread, 110.0) + 8);
+  const double e = kU * (wide ? terms + reach * 0x1p-23 : reach) + 8 * kU * largest + kU * (std::min(spread, 110.0) + 8);
   w.tol = 2 * e + (256 + 20 * ((double)(hi - lo + 1) / 64 + 2) + 30) * kU;
   return w;
 }
 
-static void compare(Rows &r, int64_t left, int64_t right, const char *what) {
+static void compare(Rows &r, int64_t left, int64_t right, const char *what, bool wide = false) {
   printf("%s: %d frames, %d new, group %d, dh %d, bits %d\n", what, r.frames, r.T, r.group, r.dh, r.bits); fflush(stdout);
   Cached c;
   fill(c, r);
@@ -108,7 +111,7 @@ static void compare(Rows &r, int64_t left, int64_t right, const char *what) {
     if (got.empty()) continue;
     double worst = 0, part = 0;
     for (int t = 0; t < r.T; ++t) for (int h = 0; h < r.group; ++h) {
-      const Want w = want_of(c, r, t, h, left, right);
+      const Want w = want_of(c, r, t, h, left, right, wide);
       for (int e = 0; e < r.dh; ++e) {
         const double d = fabs(got[((size_t)t * r.group + h) * r.dh + e] - w.o[e]) / w.mag;
         at_least(worst, d); at_least(part, d / w.tol);
@@ -234,6 +237,50 @@ static void scores() {
     scores_of(20, 1, 128, 8, q, k);
   }
 }
+// `many` query columns `ratio` times the others, where the keys are zero.
+static void outlier_query(int T, int group, int dh, int bits, float ratio, int many = 1) {
+  Rows r = make_rows(130, T, group, dh, bits);
+  for (int j = 0; j < r.frames; ++j) for (int i = 0; i < many; ++i) {
+    for (int h = 0; h < group; ++h) r.query(j, h)[3 + i] = 2.0f * ratio;
+    r.key(j)[3 + i] = 0.0f;
+  }
+  char what[64];
+  snprintf(what, sizeof what, "a query column x %g", ratio);
+  compare(r, -1, 0, what, ratio >= 300.0f);
+}
+// Rows whose column stands out beside others: the others' bits are the same as without.
+static void neighbours_of_outliers() {
+  printf("neighbours of a row with an outlier\n");
+  for (int T : {2, 4, 20}) {
+    const uint32_t start = seed;
+    std::vector<float> got[2][5];
+    for (int with = 0; with < 2; ++with) {
+      seed = start;
+      Rows r = make_rows(130, T, 1, 64, 8);
+      if (with) r.query(129, 0)[7] = 1e5f;
+      Cached c;
+      fill(c, r);
+      for (int form = 0; form < 5; ++form) got[with][form] = attend_form(c, r, -1, 0, form);
+      free(c.g.data);
+    }
+    for (int form = 0; form < 5; ++form)
+      if (!got[0][form].empty() && memcmp(got[0][form].data(), got[1][form].data(), (size_t)(T - 1) * 64 * 4)) complain("a neighbour of an outlier");
+  }
+}
+static void queries() {
+  for (float ratio : {8.0f, 64.0f, 300.0f, 1000.0f, 1e6f, 1e12f}) {
+    outlier_query(1, 2, 64, 8, ratio);
+    outlier_query(9, 2, 128, 4, ratio);
+  }
+  outlier_query(4, 1, 128, 8, 1000.0f, 5);
+  outlier_query(3, 1, 100, 8, 1e4f, 8);
+  outlier_query(17, 1, 80, 8, 1e4f, 1);
+  outlier_query(2, 1, 36, 4, 1e5f, 2);
+  outlier_query(5, 3, 20, 4, 1e4f, 1);
+  outlier_query(1, 1, 8, 8, 1e3f, 1);
+  outlier_query(20, 1, 5, 8, 1e3f, 1);
+  neighbours_of_outliers();
+}
 }  // namespace aqt
 int main(int argc, char **argv) {
   using namespace aqt;
@@ -241,6 +288,7 @@ int main(int argc, char **argv) {
   if (what == "weights") weights();
   else if (what == "nonfinite") nonfinite();
   else if (what == "scores") scores();
+  else if (what == "queries") queries();
   else complain("no such test");
   printf(bad ? "MISMATCH\n" : "ok\n");
   return bad;

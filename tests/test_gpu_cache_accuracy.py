@@ -15,12 +15,14 @@ FORMS = [(1, 256, 1, 1, 64, 8, 200, 1), (2, 256, 4, 2, 36, 4, 200, 2), (1, 256, 
          (16, 128, 8, 4, 100, 4, 120, 120)]
 
 
-def expected(ref, rows, T, left, right):
+def expected(ref, rows, T, left, right, wide=False):
     """ctx of the last T frames in float64, and what an output may be off by.  A score: the query's digits are off by half a unit of
     its largest column over 2^23, so by U max|q| sum|k| / sqrt(dh), and eight roundings of it and of its distance from the largest
     (a frame 110 below it weighs nothing, and its roundings neither); twice that in the quotient.  A weight, probability times scale: an
     integer of which the largest of a tile is 2^21 at least, so half a unit is 4 U of it, for each of 64 frames; four roundings for
-    every tile, the sum of weights sixteen.  Relative to the sum of the weights times the frames' largest values."""
+    every tile, the sum of weights sixteen.  Relative to the sum of the weights times the frames' largest values.
+    wide: rows in which a column stands out far; their digits go on for 23 bits, and what is left is the rounding of the sums, U of the
+    products' magnitudes."""
     x = rows.reshape(ref.n, T, -1, ref.dh)
     out, tol = np.zeros((ref.n, T, ref.heads, ref.dh)), np.zeros((ref.n, T, ref.heads, 1))
     g = ref.heads // ref.kv
@@ -37,6 +39,8 @@ def expected(ref, rows, T, left, right):
         out[b] = (p @ v).transpose(1, 0, 2)
         mag = (p * np.abs(v).max(2)[:, None]).sum(2)
         reach = np.abs(q).max(2) * (np.where(seen[None], np.abs(k).sum(2)[:, None], 0).max(2)) / np.sqrt(ref.dh)
+        if wide:
+            reach = np.where(seen[None], np.abs(q) @ np.abs(k).transpose(0, 2, 1), 0).max(2) / np.sqrt(ref.dh) + reach * 2.0 ** -23
         spread = np.minimum(score.max(2) - np.where(seen[None], s, np.inf).min(2), 110.0)
         e = U * reach + 8 * U * np.where(seen[None], np.abs(s), 0).max(2) + U * (spread + 8)
         tol[b, :, :, 0] = ((2 * e + (256 + 20 * (end / 64 + 2) + 30) * U) * mag).T
@@ -61,9 +65,9 @@ def run(form, change, left=-1, right=0):
     return host(B.aqt_attention_cached_fwd(dev(new), cache, T, heads, left=left, right=right)[0]), ref, new
 
 
-def compare(form, change, left=-1, right=0):
+def compare(form, change, left=-1, right=0, wide=False):
     got, ref, new = run(form, change, left, right)
-    want, tol = expected(ref, new, form[-1], left, right)
+    want, tol = expected(ref, new, form[-1], left, right, wide)
     err = np.abs(got - want)
     say("  worst", (err / (tol + 1e-30)).max(), "of its tolerance")
     assert (err <= tol + 1e-30).all()
@@ -155,3 +159,26 @@ def test_scores_of_ordinary_size_from_small_and_large_factors(form, qs, ks):
         q *= F(qs)
         k *= F(ks)
     compare(form, change)
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("ratio,many", [(300.0, 1), (1e4, 6), (1e6, 1)])
+def test_query_columns_that_stand_out(form, ratio, many):
+    """... and meet keys of zero: the other columns' scores are those of float32 sums."""
+    say("standing out", form, ratio, many)
+
+    def change(q, k, v):
+        q[..., 3:3 + many], k[..., 3:3 + many] = 2 * ratio, 0.0
+    compare(form, change, wide=True)
+
+
+@pytest.mark.parametrize("form", [f for f in FORMS if f[-1] > 1])
+def test_neighbours_of_a_row_that_stands_out(form):
+    say("neighbours", form)
+    T, heads, dh = form[-1], form[2], form[4]
+
+    def with_one(q, k, v):
+        q[:, -1, 0, 2] = 1e5
+    rows = [run(form, change)[0].reshape(-1, T, heads, dh) for change in (lambda q, k, v: None, with_one)]
+    np.testing.assert_array_equal(rows[0][:, :-1], rows[1][:, :-1])
+    np.testing.assert_array_equal(rows[0][:, -1, 1:], rows[1][:, -1, 1:])
