@@ -24,6 +24,11 @@ constexpr int kThreads = 256;
 constexpr int kBlocks = 16384;      // one row to a wavefront up to there (128 x 512 rows of 1024 columns, forward: 113 us with 2048, 97)
 constexpr int kFoldBlocks = 1024;   // where every workgroup leaves column sums behind: what fits the chip (gradient 144 us, 152 with 4096)
 constexpr int kFwdHeads = 2, kBwdHeads = 1;   // heads of a lane whose loads are in flight together (two backward: 44 -> 52 us, fewer wavefronts fit)
+// Terms of a lane that are added up in float32 before they go to float64 sums: so the error of a gain's gradient does not grow with the
+// rows (65536 rows of 8 heads: 1e-7 of it, a million: 3.6e-7 with float32 throughout).  Float64 in registers from the first term takes
+// them from the wavefronts (12800 rows of 1536, halves of 30 columns, both directions: 77 us, 90 so); handing over every 4 terms instead
+// of 8 costs where a lane has no more than that (12800 rows of 1536, whole heads rotated, both directions: 75 us, 77 so).
+constexpr int kInFloat = 8;
 constexpr int kMaxPairs = 64;                 // of the widest head
 typedef float v4f __attribute__((ext_vector_type(4)));
 
@@ -192,9 +197,10 @@ struct Apart {
   }
 };
 
-// BWD: y is the upstream gradient, out the gradient with respect to x, part (nullable) [workgroups][2][dh] column sums.
-template <class F, bool BWD>
-__global__ __launch_bounds__(kThreads) void rotate_kernel(const float *x, const float *y, RotateGeom g, float *out, float *part) {
+// BWD: y is the upstream gradient, out the gradient with respect to x; GAINS: part [workgroups][2][dh] column sums (a kernel of its own,
+// for the registers of their sums: 32 x 400 rows of 1536 columns without them 33 us, and 36 in a kernel for both).
+template <class F, bool BWD, bool GAINS = BWD>
+__global__ __launch_bounds__(kThreads, GAINS ? 4 : 1) void rotate_kernel(const float *x, const float *y, RotateGeom g, float *out, float *part) {
   constexpr int L = F::LANES, N = F::N, GROUPS = 64 / L, U = BWD ? kBwdHeads : kFwdHeads, PAIRS = F::PAIRS;
   const int tid = static_cast<int>(threadIdx.x), lane = tid & 63, group = lane / L, j = lane % L;
   const F f(j, g.dh, g.rot);
@@ -215,12 +221,31 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const float *x, const 
   const int row_lanes = L * g.per_row, place = sub * L + j;
   Angle *const row_angles = angles[tid >> 6] + row_of * PAIRS;
   float *const head = F::SCRATCH > 4 ? heads[tid >> 6] + group * 8 * L : nullptr;
-  float dgain[2][N];   // only where it is asked for (BWD)
+  float dgain[2][N];   // GAINS
 #pragma unroll
   for (int w = 0; w < 2; ++w)
 #pragma unroll
     for (int i = 0; i < N; ++i) dgain[w][i] = 0.0f;
+  __shared__ double sums[kThreads / 64][2][GAINS ? 128 : 1];
+  if (GAINS)
+    for (int i = tid; i < kThreads / 64 * 2 * 128; i += kThreads) (&sums[0][0][0])[i] = 0.0;
   __syncthreads();
+  // What the lanes have added up, over the groups of the wavefront, to its sums in float64.
+  auto hand_over = [&] {
+#pragma unroll
+    for (int w = 0; w < 2; ++w)
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        float s = dgain[w][i];
+#pragma unroll
+        for (int off = L; off < 64; off <<= 1) s += __shfl_xor(s, off, 64);
+        if (group == 0 && f.own(i)) sums[tid >> 6][w][f.column(i)] += static_cast<double>(s);
+        dgain[w][i] = 0.0f;
+        __builtin_amdgcn_sched_barrier(0);   // one after the other: side by side they take registers from the rows
+      }
+  };
+  int in_float = 0;
+  const int steps = (g.heads + g.per_row - 1) / g.per_row;
 
   // All wavefronts walk the rows side by side: what is in flight at a time is one piece of memory
   // (32 x 400 rows of 1536 columns, forward, with a run of rows to each instead: 32 us, 26.5 so).
@@ -302,8 +327,10 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const float *x, const 
             for (int i = 0; i < N; ++i) {
               v[k][i] *= r;
               const float mine = on && !value ? u[i] * v[k][i] : 0.0f;
-              dgain[0][i] += query ? mine : 0.0f;
-              dgain[1][i] += query ? 0.0f : mine;
+              if (GAINS) {
+                dgain[0][i] += query ? mine : 0.0f;
+                dgain[1][i] += query ? 0.0f : mine;
+              }
               u[i] *= gain[i];
               dot = fmaf(u[i], v[k][i], dot);
             }
@@ -317,6 +344,10 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const float *x, const 
         if (on) f.store(u, outr + static_cast<int64_t>(h) * g.dh);
       }
     }
+    if (GAINS && (in_float += steps) >= kInFloat) {
+      in_float = 0;
+      hand_over();
+    }
     b += g.stride_b;
     t += g.stride_t;
     if (t >= g.T) {
@@ -324,25 +355,14 @@ __global__ __launch_bounds__(kThreads) void rotate_kernel(const float *x, const 
       ++b;
     }
   }
-  if constexpr (BWD) {
-    if (!part) return;
-    // over the groups of the wavefront, then over the wavefronts
-    __shared__ float sums[kThreads / 64][2][128];
-#pragma unroll
-    for (int w = 0; w < 2; ++w)
-#pragma unroll
-      for (int i = 0; i < N; ++i) {
-        float s = dgain[w][i];
-#pragma unroll
-        for (int off = L; off < 64; off <<= 1) s += __shfl_xor(s, off, 64);
-        if (group == 0 && f.own(i)) sums[tid >> 6][w][f.column(i)] = s;
-      }
+  if constexpr (GAINS) {
+    hand_over();
     __syncthreads();
     if (tid < 2 * g.dh) {
       const int w = tid >= g.dh, c = w ? tid - g.dh : tid;
-      float s = 0.0f;
+      double s = 0.0;
       for (int k = 0; k < kThreads / 64; ++k) s += sums[k][w][c];
-      part[static_cast<int64_t>(blockIdx.x) * 2 * g.dh + tid] = s;
+      part[static_cast<int64_t>(blockIdx.x) * 2 * g.dh + tid] = static_cast<float>(s);
     }
   }
 }
@@ -394,7 +414,11 @@ aqt_status launch_as(const float *x, const float *y, RotateGeom g, float *out, f
   g.stride = static_cast<int64_t>(*blocks) * (kThreads / 64) * rows_at_once;
   g.stride_b = g.stride / g.T;
   g.stride_t = g.stride % g.T;
-  rotate_kernel<F, BWD><<<*blocks, kThreads, 0, st>>>(x, y, g, out, part);
+  // The gradient without gains' has registers for seven wavefronts to a SIMD, but memory is better served by the streams of five, whose
+  // workgroups this much LDS leaves room for (128 x 512 rows of 1024 columns: 137 us with seven, 130 so; smaller calls equal).
+  constexpr size_t kRoom = 20480;
+  auto kern = part ? rotate_kernel<F, BWD, BWD> : rotate_kernel<F, BWD, false>;   // (forward: the same)
+  kern<<<*blocks, kThreads, BWD && !part ? kRoom : 0, st>>>(x, y, g, out, part);
   AQT_HIP(hipGetLastError());
   return AQT_OK;
 }

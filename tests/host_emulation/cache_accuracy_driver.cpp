@@ -281,6 +281,34 @@ static void queries() {
   outlier_query(20, 1, 5, 8, 1e3f, 1);
   neighbours_of_outliers();
 }
+// Gains' gradients over many rows of a lane: the first of each a term of 1, the others 2^-25 and a little less, which a float32 sum
+// would lose one by one.  Of a term 16 steps; eight terms of a lane, its groups' sums, the workgroup's word and the result.
+static void gains_of_many_rows(int64_t T, int dh, bool vec) {
+  const int heads = 1, kv = 1, cols = 3 * dh, L = dh <= 32 ? 4 : dh <= 64 ? 8 : 16;
+  const int per_row = std::min(64 / L, 4), stride = 4 * (64 / L / per_row);   // rows that the one workgroup takes at a time
+  printf("gains of %ld rows, dh %d, %ld to a lane\n", (long)T, dh, (long)(T / stride)); fflush(stdout);
+  std::vector<float> x((size_t)T * cols, 1.0f), dy((size_t)T * cols), dx((size_t)T * cols), part(2 * dh), dgq(dh), dgk(dh);
+  double want = 0;
+  for (int64_t m = 0; m < T; ++m) {
+    const float t = m < stride ? 1.0f : 0.9f * 0x1p-25f;
+    for (int c = 0; c < cols; ++c) dy[(size_t)m * cols + c] = t;
+    want += t / sqrt(1.0 + 1e-6);
+  }
+  turn::RotateGeom g{};
+  g.T = T; g.M = T; g.ld = cols; g.heads = heads; g.kv_heads = kv; g.dh = dh; g.norm = 1; g.eps = 1e-6f;
+  turn_paired<false, true>(x.data(), dy.data(), g, dx.data(), part.data(), vec ? 2 : 0, 1);
+  run((unsigned)((2 * dh + 15) / 16), turn::kFoldThreads, 0, [&] { turn::rotate_fold_kernel(part.data(), 1, dh, dgq.data(), dgk.data()); });
+  double worst = 0;
+  for (int c = 0; c < dh; ++c) { at_least(worst, fabs(dgq[c] - want) / want); at_least(worst, fabs(dgk[c] - want) / want); }
+  printf("  worst error %.3g\n", worst);
+  if (!(worst <= (16 + 8 + 4 + 1 + 1) * kU)) complain("gains of many rows");
+}
+static void gains() {
+  gains_of_many_rows(16 * 250 + 3, 8, true);
+  gains_of_many_rows(8 * 250, 7, false);
+  gains_of_many_rows(8 * 200, 36, true);
+  gains_of_many_rows(4 * 200, 101, false);
+}
 }  // namespace aqt
 int main(int argc, char **argv) {
   using namespace aqt;
@@ -289,6 +317,7 @@ int main(int argc, char **argv) {
   else if (what == "nonfinite") nonfinite();
   else if (what == "scores") scores();
   else if (what == "queries") queries();
+  else if (what == "gains") gains();
   else complain("no such test");
   printf(bad ? "MISMATCH\n" : "ok\n");
   return bad;

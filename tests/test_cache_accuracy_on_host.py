@@ -22,7 +22,7 @@ def exe(tmp_path_factory):
     return str(path / "cache")
 
 
-@pytest.mark.parametrize("what", ["weights", "nonfinite", "scores", "queries"])
+@pytest.mark.parametrize("what", ["weights", "nonfinite", "scores", "queries", "gains"])
 def test_as_the_formula_says(exe, what):
     r = subprocess.run([exe, what], capture_output=True, text=True, env=dict(os.environ, ASAN_OPTIONS="detect_leaks=0"), timeout=900)
     assert r.returncode == 0 and r.stdout.strip().endswith("ok"), (r.stdout[-3000:], r.stderr[-3000:])
