@@ -627,7 +627,7 @@ aqt_status aqt_conformer_layer_bwd(const float *dy, const float *x, const aqt_co
 typedef struct aqt_qk_norm_rotate {
   int heads, kv_heads, dh;   /* kv_heads divides heads; dh <= 128               */
   int norm;                  /* 0: rotation only                                */
-  float eps;                 /* >= 0                                            */
+  float eps;                 /* >= 0; 0: a head of zeros gives NaN              */
   int rot, pairing;          /* even, 0 .. dh; AQT_ROTATE_*                     */
   const float *gamma_q;      /* nullable [dh]                                   */
   const float *gamma_k;      /* nullable [dh]                                   */

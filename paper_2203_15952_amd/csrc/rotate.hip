@@ -197,6 +197,28 @@ struct Apart {
   }
 };
 
+// 1 / rms of a head from a lane's columns v.  Heads whose squares float32 does not hold (their mean and eps under 2^-100, of which
+// the instruction takes what lies under 2^-126 for zeros, or infinite) are scaled by a power of two first, v with them: by h h, and 1 / rms
+// is h h times the result.  A branch that the wavefront steps over where none of its heads is such.
+template <int L, int N>
+__device__ __forceinline__ float inverse_rms(float (&v)[N], float inv, float eps, float &h) {
+  auto mean = [&] {
+    float ss = 0.0f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) ss = fmaf(v[i], v[i], ss);
+    return group_sum<L>(ss) * inv;
+  };
+  float m = mean() + eps;
+  h = 1.0f;
+  if (__any(!(m >= 0x1p-100f && m < __builtin_inff()))) {
+    h = m >= 0x1p-100f && m < __builtin_inff() ? 1.0f : m < 0x1p-100f ? 0x1p48f : 0x1p-48f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] *= h * h;
+    m = mean() + eps * (h * h) * (h * h);
+  }
+  return __builtin_amdgcn_rsqf(m);
+}
+
 // BWD: y is the upstream gradient, out the gradient with respect to x; GAINS: part [workgroups][2][dh] column sums (a kernel of its own,
 // for the registers of their sums: 32 x 400 rows of 1536 columns without them 33 us, and 36 in a kernel for both).
 template <class F, bool BWD, bool GAINS = BWD>
@@ -298,13 +320,13 @@ __global__ __launch_bounds__(kThreads, GAINS ? 4 : 1) void rotate_kernel(const f
           for (int i = 0; i < N; ++i) u[i] = BWD ? w[k][i] : v[k][i];
         } else if (!BWD) {
           if (g.norm) {
-            float gain[N], ss = 0.0f;
+            float gain[N], x[N], half_scale;
             f.load_gains(gain, gains[query ? 0 : 1]);
 #pragma unroll
-            for (int i = 0; i < N; ++i) ss = fmaf(v[k][i], v[k][i], ss);
-            const float r = __builtin_amdgcn_rsqf(group_sum<L>(ss) * inv + g.eps);
+            for (int i = 0; i < N; ++i) x[i] = v[k][i];
+            const float r = inverse_rms<L>(x, inv, g.eps, half_scale);
 #pragma unroll
-            for (int i = 0; i < N; ++i) u[i] = v[k][i] * r * gain[i];
+            for (int i = 0; i < N; ++i) u[i] = x[i] * r * gain[i];
           } else {
 #pragma unroll
             for (int i = 0; i < N; ++i) u[i] = v[k][i];
@@ -317,11 +339,9 @@ __global__ __launch_bounds__(kThreads, GAINS ? 4 : 1) void rotate_kernel(const f
           for (int i = 0; i < N; ++i) u[i] = w[k][i];
           f.turn(u, a, true, head);
           if (g.norm) {
-            float gain[N], ss = 0.0f;
+            float gain[N], half_scale;
             f.load_gains(gain, gains[query ? 0 : 1]);
-#pragma unroll
-            for (int i = 0; i < N; ++i) ss = fmaf(v[k][i], v[k][i], ss);
-            const float r = __builtin_amdgcn_rsqf(group_sum<L>(ss) * inv + g.eps);
+            const float r = inverse_rms<L>(v[k], inv, g.eps, half_scale);
             float dot = 0.0f;
 #pragma unroll
             for (int i = 0; i < N; ++i) {
@@ -336,7 +356,14 @@ __global__ __launch_bounds__(kThreads, GAINS ? 4 : 1) void rotate_kernel(const f
             }
             dot = group_sum<L>(dot) * inv;
 #pragma unroll
-            for (int i = 0; i < N; ++i) u[i] = (u[i] - v[k][i] * dot) * r;
+            for (int i = 0; i < N; ++i) u[i] -= v[k][i] * dot;
+            if (__any(half_scale != 1.0f)) {   // one half in front of r, one behind: the product in between stays a number
+#pragma unroll
+              for (int i = 0; i < N; ++i) u[i] = u[i] * half_scale * r * half_scale;
+            } else {
+#pragma unroll
+              for (int i = 0; i < N; ++i) u[i] *= r;
+            }
           }
 #pragma unroll
           for (int i = 0; i < N; ++i) u[i] = value ? w[k][i] : u[i];

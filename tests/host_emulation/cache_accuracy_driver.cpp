@@ -309,6 +309,64 @@ static void gains() {
   gains_of_many_rows(8 * 200, 36, true);
   gains_of_many_rows(4 * 200, 101, false);
 }
+// Heads of any size without an epsilon, one head of each size in a row: columns whose squares float32 does not hold.  Rounding steps of
+// 2^-24 as in the tests of ordinary heads: 18 forward, 48 for the gradient, each of the magnitudes of its pair.
+static void rotate_sizes(int dh, int rot, bool halves, bool vec, std::vector<float> sizes, float eps) {
+  const int heads = (int)sizes.size(), kv = 1, cols = (heads + 2) * dh, np = rot / 2;
+  const int64_t T = 5;
+  printf("heads of all sizes, dh %d, rot %d, halves %d, eps %g\n", dh, rot, halves, eps); fflush(stdout);
+  std::vector<float> x((size_t)T * cols), dy(x.size()), out(x.size()), dx(x.size()), part(2 * dh), gq(dh), dgq(dh), dgk(dh);
+  for (int64_t m = 0; m < T; ++m) for (int h = 0; h < heads + 2; ++h) for (int i = 0; i < dh; ++i) {
+    const float s = h < heads ? sizes[h] : 1.0f;
+    x[m * cols + h * dh + i] = s * uniform();
+    dy[m * cols + h * dh + i] = s * uniform();   // a gradient of the head's own size: that of x is about 1
+  }
+  for (float &v : gq) v = 1.0f + 0.3f * uniform();
+  std::vector<double> turns(np ? np : 1);
+  for (int i = 0; i < np; ++i) turns[i] = pow(10000.0, -(double)i / np) / (2 * M_PI);
+  turn::RotateGeom g{};
+  g.T = T; g.M = T; g.ld = cols; g.heads = heads; g.kv_heads = kv; g.dh = dh; g.rot = rot; g.norm = 1; g.eps = eps; g.turns = turns.data(); g.gamma[0] = gq.data();
+  const int form = vec ? (!halves || rot % 8 == 0 ? 2 : 1) : 0;
+  if (halves) { turn_paired<true, false>(x.data(), nullptr, g, out.data(), nullptr, form, 1); turn_paired<true, true>(x.data(), dy.data(), g, dx.data(), part.data(), form, 1); }
+  else { turn_paired<false, false>(x.data(), nullptr, g, out.data(), nullptr, form, 1); turn_paired<false, true>(x.data(), dy.data(), g, dx.data(), part.data(), form, 1); }
+  double worst = 0, worst_dx = 0;
+  for (int64_t m = 0; m < T; ++m) for (int h = 0; h < heads; ++h) {
+    const float *xr = &x[m * cols + h * dh], *dr = &dy[m * cols + h * dh], *o = &out[m * cols + h * dh], *d = &dx[m * cols + h * dh];
+    double ss = 0;
+    for (int i = 0; i < dh; ++i) ss += (double)xr[i] * xr[i];
+    const double r = 1.0 / sqrt(ss / dh + (double)eps);
+    std::vector<double> u(dh), um(dh), w(dh), wm(dh);
+    for (int i = 0; i < dh; ++i) { u[i] = xr[i] * r * gq[i]; um[i] = fabs(u[i]); w[i] = dr[i]; wm[i] = fabs(w[i]); }
+    for (int p = 0; p < np; ++p) {
+      const int a = halves ? p : 2 * p, b = halves ? p + np : 2 * p + 1;
+      const double an = 2 * M_PI * m * turns[p], cc = cos(an), s = sin(an), ua = u[a], ub = u[b], wa = w[a], wb = w[b];
+      u[a] = ua * cc - ub * s; u[b] = ua * s + ub * cc; w[a] = wa * cc + wb * s; w[b] = wb * cc - wa * s;
+      um[a] = um[b] = um[a] + um[b]; wm[a] = wm[b] = wm[a] + wm[b];
+    }
+    // A gradient of 3e38: |a cos| + |b sin| reaches 3e38 sqrt(2) = 4.2e38, and times a gain of 1.3 5.5e38, where float32 ends at
+    // 3.4e38: the rotated gradient itself is no number, and neither is what is made of it.
+    bool beyond = false;
+    for (int i = 0; i < dh; ++i) beyond = beyond || wm[i] * fabs(gq[i]) > 3.4e38;
+    double dot = 0, dotm = 0;
+    for (int i = 0; i < dh; ++i) { dot += w[i] * gq[i] * xr[i] * r; dotm += wm[i] * fabs(gq[i] * xr[i] * r); }
+    for (int i = 0; i < dh; ++i) {
+      at_least(worst, fabs(o[i] - u[i]) / (18 * kU * um[i] + 1e-30));
+      // (gradients next to the smallest numbers have these as steps)
+      if (!beyond) at_least(worst_dx, fabs(d[i] - (w[i] * gq[i] - xr[i] * r * dot / dh) * r) / (48 * kU * r * (wm[i] * fabs(gq[i]) + fabs(xr[i] * r) * dotm / dh) + 0x1p-149 * r * dh + 1e-30));
+    }
+  }
+  printf("  worst of their tolerances: out %.3g dx %.3g\n", worst, worst_dx);
+  if (!(worst <= 1.0) || !(worst_dx <= 1.0)) complain("heads of all sizes");
+}
+static void sizes() {
+  const std::vector<float> all = {1.0f, 1e-20f, 3e-38f, 1e20f, 1e-10f, 3e38f, 1e-30f, 1e15f};
+  rotate_sizes(64, 64, true, true, all, 0.0f);
+  rotate_sizes(36, 36, false, true, all, 0.0f);
+  rotate_sizes(20, 20, true, true, all, 0.0f);
+  rotate_sizes(101, 100, true, false, all, 0.0f);
+  rotate_sizes(128, 64, true, true, all, 1e-35f);
+  rotate_sizes(8, 4, false, false, {1e20f, 1.0f, 1e19f}, 1e-6f);
+}
 }  // namespace aqt
 int main(int argc, char **argv) {
   using namespace aqt;
@@ -318,6 +376,7 @@ int main(int argc, char **argv) {
   else if (what == "scores") scores();
   else if (what == "queries") queries();
   else if (what == "gains") gains();
+  else if (what == "sizes") sizes();
   else complain("no such test");
   printf(bad ? "MISMATCH\n" : "ok\n");
   return bad;
