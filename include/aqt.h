@@ -639,7 +639,7 @@ aqt_status aqt_rotation_turns(int rot, double base, double *turns, void *stream)
 
 /*
  * out [B*T, (heads + 2 kv_heads) dh]: rotated queries and keys, values as they are.  out may be
- * qkv itself (the values are then not touched), but not overlap it otherwise.
+ * qkv itself (the values are then not touched), but not overlap it, or what else the call reads, otherwise.
  */
 aqt_status aqt_qk_norm_rotate_fwd(const float *qkv, int64_t B, int64_t T, const aqt_qk_norm_rotate *spec,
                                   const int64_t *first, float *out, void *stream);
@@ -666,7 +666,8 @@ aqt_status aqt_qk_norm_rotate_bwd(const float *qkv, const float *dout, int64_t B
  *   first ones; NULL: all; values outside 0..T count as the nearest).  What belongs to the other
  *   rows is neither read nor written.
  * Lengths and counts live on the device: nothing in these calls waits for them, and a captured
- * step follows them from replay to replay.  The buffer needs no clearing.
+ * step follows them from replay to replay.  The buffer needs no clearing.  What a call writes (results,
+ * workspace, the cache) may overlap neither what it reads nor each other; such calls are refused.
  */
 typedef struct aqt_cache {
   int64_t streams;

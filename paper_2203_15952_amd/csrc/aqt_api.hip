@@ -1118,6 +1118,9 @@ aqt_status aqt_qk_norm_rotate_fwd(const float *qkv, int64_t B, int64_t T, const 
   if (!qkv || !out) return AQT_ERR_INVALID_ARG;
   const size_t bytes = rotate_row_bytes(*spec) * B * T;
   if (out != qkv && overlap(qkv, bytes, out, bytes)) return AQT_ERR_INVALID_ARG;
+  const size_t head = spec->dh * sizeof(float);
+  if (!apart({{out, bytes}}, {{spec->gamma_q, head}, {spec->gamma_k, head}, {spec->turns, spec->rot / 2 * sizeof(double)}, {first, B * sizeof(int64_t)}}))
+    return AQT_ERR_INVALID_ARG;
   return launch_rotate_fwd(qkv, B, T, *spec, first, out, static_cast<hipStream_t>(stream));
 }
 
@@ -1130,13 +1133,18 @@ aqt_status aqt_qk_norm_rotate_bwd(const float *qkv, const float *dout, int64_t B
   const size_t bytes = rotate_row_bytes(*spec) * B * T;
   if ((dqkv != dout && overlap(dout, bytes, dqkv, bytes)) || overlap(qkv, spec->norm ? bytes : 0, dqkv, bytes)) return AQT_ERR_INVALID_ARG;
   if (gains && (!ws || ws_bytes < rotate_bwd_ws_bytes(spec->dh))) return AQT_ERR_WORKSPACE;
+  const size_t head = spec->dh * sizeof(float);
+  const Span small[] = {{dgamma_q, head}, {dgamma_k, head}, {gains ? ws : nullptr, rotate_bwd_ws_bytes(spec->dh)}};
+  if (!apart({{dqkv, bytes}, small[0], small[1], small[2]}, {{spec->gamma_q, head}, {spec->gamma_k, head},
+              {spec->turns, spec->rot / 2 * sizeof(double)}, {first, B * sizeof(int64_t)}}) ||
+      !apart({small[0], small[1], small[2]}, {{spec->norm ? qkv : nullptr, bytes}, {dout, bytes}}))   // dqkv: above
+    return AQT_ERR_INVALID_ARG;
   return launch_rotate_bwd(qkv, dout, B, T, *spec, first, dqkv, dgamma_q, dgamma_k, ws, static_cast<hipStream_t>(stream));
 }
 
 size_t aqt_cache_bytes(const aqt_cache *shape) {
   if (cache_check(shape) != AQT_OK) return 0;
-  const CacheGeom g = cache_geom(*shape);
-  return static_cast<size_t>(g.streams) * g.kv_heads * g.tiles * g.tile_bytes;
+  return cache_bytes(cache_geom(*shape));
 }
 
 aqt_status aqt_cache_append(const float *qkv, int64_t T, int heads, const aqt_cache *cache, const int32_t *count, void *stream,
@@ -1158,6 +1166,7 @@ aqt_status aqt_cache_read(const aqt_cache *cache, int64_t pending, const int32_t
 aqt_status aqt_cache_advance(int64_t *length, int64_t streams, int64_t T, const int32_t *count, void *stream) {
   if (!length || streams < 1 || T < 1) return AQT_ERR_INVALID_ARG;
   if (streams > (int64_t(1) << 24) || T > (int64_t(1) << 40)) return AQT_ERR_UNSUPPORTED;
+  if (overlap(length, streams * sizeof(int64_t), count, streams * sizeof(int32_t))) return AQT_ERR_INVALID_ARG;
   return launch_cache_advance(length, streams, T, count, static_cast<hipStream_t>(stream));
 }
 
@@ -1173,9 +1182,15 @@ aqt_status aqt_attention_cached_fwd(const float *qkv, int64_t T, int heads, cons
   AQT_TRY(cache_call_check(cache, T, heads));
   if (!qkv || !ctx) return AQT_ERR_INVALID_ARG;
   if (!cached_attention_ok(*cache, T, heads)) return AQT_ERR_UNSUPPORTED;
-  const size_t rows = static_cast<size_t>(cache->streams) * T * cache->dh * sizeof(float);
-  if (overlap(qkv, rows * (heads + 2 * static_cast<size_t>(cache->kv_heads)), ctx, rows * heads)) return AQT_ERR_INVALID_ARG;
-  if (!ws || ws_bytes < cached_attention_ws_bytes(*cache, T, heads)) return AQT_ERR_WORKSPACE;
+  const CacheGeom g = cache_geom(*cache);
+  const size_t streams = static_cast<size_t>(g.streams);
+  const Span qkv_span = {qkv, cache_rows_bytes(g, T, heads)}, ctx_span = {ctx, streams * T * heads * g.dh * sizeof(float)};
+  if (!apart({ctx_span}, {qkv_span})) return AQT_ERR_INVALID_ARG;
+  const size_t need = cached_attention_ws_bytes(*cache, T, heads);
+  if (!ws || ws_bytes < need) return AQT_ERR_WORKSPACE;
+  if (!apart({ctx_span, {ctx_absmax, sizeof(float)}, {ws, need}},
+             {qkv_span, {g.data, cache_bytes(g)}, {g.length, streams * sizeof(int64_t)}, {count, streams * sizeof(int32_t)}}))
+    return AQT_ERR_INVALID_ARG;
   return launch_attention_cached(qkv, T, heads, *cache, count, left_context, right_context, ctx,
                                  reinterpret_cast<uint32_t *>(ctx_absmax), ws, static_cast<hipStream_t>(stream));
 }

@@ -3,6 +3,7 @@
 
 #include <hip/hip_runtime.h>
 #include <stdint.h>
+#include <initializer_list>
 
 #include "aqt.h"
 
@@ -68,6 +69,21 @@ __device__ __forceinline__ void wave_lds_order() {
 inline bool overlap(const void *a, size_t n, const void *b, size_t m) {
   const uintptr_t p = reinterpret_cast<uintptr_t>(a), q = reinterpret_cast<uintptr_t>(b);
   return a && b && p < q + m && q < p + n;
+}
+
+// Pieces of memory that a call writes, and that it reads: none of the former may overlap another of either.
+struct Span {
+  const void *at;   // nullable
+  size_t bytes;
+};
+inline bool apart(std::initializer_list<Span> written, std::initializer_list<Span> read) {
+  for (const Span *w = written.begin(); w != written.end(); ++w) {
+    for (const Span &r : read)
+      if (w->bytes && r.bytes && overlap(w->at, w->bytes, r.at, r.bytes)) return false;
+    for (const Span *v = w + 1; v != written.end(); ++v)
+      if (w->bytes && v->bytes && overlap(w->at, w->bytes, v->at, v->bytes)) return false;
+  }
+  return true;
 }
 
 inline int qmax_of(int bits) { return (1 << (bits - 1)) - 1; }

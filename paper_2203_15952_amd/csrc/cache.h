@@ -53,6 +53,14 @@ __host__ __device__ inline StreamFrames stream_frames(const CacheGeom &g, const 
 
 constexpr int64_t kMostBlocks = (int64_t(1) << 24) - 1;   // of 256 threads: a launch's threads count in 32 bits
 
+inline size_t cache_bytes(const CacheGeom &g) { return static_cast<size_t>(g.streams) * g.kv_heads * g.tiles * g.tile_bytes; }
+// Of the rows of a call, as many as an address space holds at most.
+inline size_t cache_rows_bytes(const CacheGeom &g, int64_t T, int heads) {
+  const size_t row = (static_cast<size_t>(heads) + 2 * static_cast<size_t>(g.kv_heads)) * g.dh * sizeof(float) * static_cast<size_t>(g.streams);
+  const size_t most = size_t(1) << 60;   // (row: at most 2^24 streams of 2^30 bytes)
+  return static_cast<size_t>(T) > most / row ? most : row * static_cast<size_t>(T);
+}
+
 bool cache_shape_ok(const aqt_cache &c);
 CacheGeom cache_geom(const aqt_cache &c);
 aqt_status launch_cache_append(const float *qkv, int64_t T, int heads, const aqt_cache &c, const int32_t *count, hipStream_t st,

@@ -345,6 +345,10 @@ aqt_status launch_cache_append(const float *qkv, int64_t T, int heads, const aqt
   const CacheGeom g = cache_geom(c);
   const int64_t most = T < c.capacity ? T : c.capacity;
   if (!grid_ok(g, most)) return AQT_ERR_UNSUPPORTED;
+  const size_t streams = static_cast<size_t>(g.streams);
+  if (!apart({{g.data, cache_bytes(g)}, {dev_status, sizeof(int32_t)}},
+             {{qkv, cache_rows_bytes(g, T, heads)}, {g.length, streams * sizeof(int64_t)}, {count, streams * sizeof(int32_t)}}))
+    return AQT_ERR_INVALID_ARG;
   const Cut cut = cut_of(g, most);
   const bool vec = reinterpret_cast<uintptr_t>(qkv) % 16 == 0 && c.dh % 4 == 0;
   auto kern = c.dh <= 32   ? (vec ? cache_append_kernel<4, true> : cache_append_kernel<4, false>)
@@ -360,6 +364,10 @@ aqt_status launch_cache_read(const aqt_cache &c, int64_t pending, const int32_t 
                              float *values, hipStream_t st) {
   const CacheGeom g = cache_geom(c);
   if (!grid_ok(g, n)) return AQT_ERR_UNSUPPORTED;
+  const size_t streams = static_cast<size_t>(g.streams), bytes = streams * n * g.kv_heads * g.dh * sizeof(float);
+  if (!apart({{keys, bytes}, {values, bytes}}, {{g.data, cache_bytes(g)}, {g.length, streams * sizeof(int64_t)},
+                                                {count, streams * sizeof(int32_t)}, {first, streams * sizeof(int64_t)}}))
+    return AQT_ERR_INVALID_ARG;
   const Cut cut = cut_of(g, n);
   const bool vec = reinterpret_cast<uintptr_t>(keys) % 16 == 0 && reinterpret_cast<uintptr_t>(values) % 16 == 0 && c.dh % 4 == 0;
   auto kern = c.dh <= 32   ? (vec ? cache_read_kernel<4, true> : cache_read_kernel<4, false>)
