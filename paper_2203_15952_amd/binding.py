@@ -909,14 +909,15 @@ class QkNormRotate:
     """How queries and keys of rows with `heads` queries, `kv_heads` keys and values of dh columns are normalised and rotated
     (aqt_qk_norm_rotate_fwd / _bwd), and its aqt_qk_norm_rotate view.  rot: leading columns of a head that are rotated (default:
     all that make pairs); base: of the geometric series of angles, or turns, float64 [rot / 2] turns per frame, in its place.
-    gamma_q / gamma_k: float32 [dh] on the device, kept by reference (an optimizer may change them in place)."""
+    gamma_q / gamma_k: float32 [dh] on the device, kept by reference (an optimizer may change them in place, never put others in
+    their place)."""
 
     def __init__(self, heads: int, kv_heads: int, dh: int, *, rot: Optional[int] = None, base: float = 10000.0, turns=None,
                  pairing: int = AQT_ROTATE_HALVES, norm: bool = True, eps: float = 1e-6, gamma_q=None, gamma_k=None, device="cuda"):
         self.heads, self.kv_heads, self.dh, self.norm = heads, kv_heads, dh, bool(norm)
         rot = dh // 2 * 2 if rot is None else rot
         self.columns = (heads + 2 * kv_heads) * dh
-        self.gamma_q, self.gamma_k = gamma_q, gamma_k
+        self._gamma_q, self._gamma_k = gamma_q, gamma_k
         for name, t in (("gamma_q", gamma_q), ("gamma_k", gamma_k)):
             if t is not None:
                 _shaped(t, torch.float32, (dh,), _current(t, name), name)
@@ -926,12 +927,24 @@ class QkNormRotate:
             turns = torch.empty(max(rot // 2, 1), dtype=torch.float64, device=device)
             _current(turns, "device")
             _check(lib().aqt_rotation_turns(rot, base, _ptr(turns), _stream()), "aqt_rotation_turns")
-        self.turns = turns
+        self._turns = turns
         self.device = next((t.get_device() for t in (turns, gamma_q, gamma_k) if t is not None), None)   # all on the current one
         self.c = aqt_qk_norm_rotate(heads, kv_heads, dh, int(self.norm), eps, rot, pairing,
                                     None if gamma_q is None else gamma_q.data_ptr(), None if gamma_k is None else gamma_k.data_ptr(),
                                     None if turns is None else turns.data_ptr())
         self.ref = ctypes.byref(self.c)
+
+    @property
+    def gamma_q(self) -> Optional[torch.Tensor]:
+        return self._gamma_q
+
+    @property
+    def gamma_k(self) -> Optional[torch.Tensor]:
+        return self._gamma_k
+
+    @property
+    def turns(self) -> Optional[torch.Tensor]:
+        return self._turns
 
     def on(self, device: int):
         if self.device is not None and self.device != device:

@@ -56,3 +56,15 @@ def test_heads_of_all_sizes(dh, rot, pairing, shift, eps):
     fits = np.repeat(np.abs(dy.reshape(B_ * T, 10, dh)).sum(2, dtype=np.float64) < 3.4e38, dh, axis=1)
     assert fits.reshape(B_ * T, 10, dh)[:, np.arange(10) != 5].all()
     assert (np.abs(dx - ref) <= BWD_STEPS * U * mag + slack + 1e-30)[fits].all()
+
+
+def test_gains_change_in_place_only():
+    """An optimizer's step changes them under the spec; another tensor in their place would leave it with freed memory."""
+    g = torch.ones(8, device="cuda")
+    spec, x = B.QkNormRotate(1, 1, 8, rot=0, gamma_q=g), torch.ones((1, 24), device="cuda")
+    before = B.aqt_qk_norm_rotate_fwd(x, 1, 1, spec)
+    with pytest.raises(AttributeError):
+        spec.gamma_q = torch.ones(8, device="cuda")
+    g.mul_(2.0)
+    after = B.aqt_qk_norm_rotate_fwd(x, 1, 1, spec)
+    assert torch.equal(after[:, :8], 2 * before[:, :8]) and torch.equal(after[:, 8:], before[:, 8:])
