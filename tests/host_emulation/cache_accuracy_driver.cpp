@@ -363,6 +363,7 @@ static void sizes() {
   rotate_sizes(64, 64, true, true, all, 0.0f);
   rotate_sizes(36, 36, false, true, all, 0.0f);
   rotate_sizes(20, 20, true, true, all, 0.0f);
+  rotate_sizes(100, 100, true, true, all, 0.0f);
   rotate_sizes(101, 100, true, false, all, 0.0f);
   rotate_sizes(128, 64, true, true, all, 1e-35f);
   rotate_sizes(8, 4, false, false, {1e20f, 1.0f, 1e19f}, 1e-6f);

@@ -5,8 +5,21 @@ import torch
 
 from paper_2203_15952_amd import binding as B
 from test_gpu_rotate import BWD_STEPS, F, FWD_STEPS, U, Plain, dev, host
+from test_gpu_rotate import test_backward as check_backward
+from test_gpu_rotate import test_forward as check_forward
 
 pytestmark = pytest.mark.gpu
+
+
+# whole 16-byte pieces whose rotated halves are none: heads of each width that has a kernel of its own
+PIECES_APART = [(3, 11, 4, 2, 20, 20, 0, True, True, [0, 5, 100000]), (2, 33, 3, 3, 28, 12, 0, True, True, None), (2, 17, 8, 2, 64, 62, 0, True, True, None),
+                (2, 19, 6, 2, 100, 100, 0, True, True, [7, 0]), (1, 70, 2, 1, 128, 124, 0, False, False, None)]
+
+
+@pytest.mark.parametrize("case", PIECES_APART)
+def test_pieces_whose_halves_are_none(case):
+    check_forward(case)
+    check_backward(case)
 
 
 @pytest.mark.parametrize("dh", [8, 7])
