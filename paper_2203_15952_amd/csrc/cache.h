@@ -26,7 +26,7 @@ struct CacheGeom {
   const int64_t *length;         // frames of every stream in front of the call's
 };
 
-__host__ __device__ inline int cache_keys(const CacheGeom &) { return 0; }
+// Bytes from a tile's start, where its keys are.
 __host__ __device__ inline int cache_values(const CacheGeom &g) { return 64 * g.key_row; }
 __host__ __device__ inline int cache_scales(const CacheGeom &g) { return 64 * (g.key_row + g.value_rows); }   // keys', then values'
 __host__ __device__ inline int frame_slot(int frame) { return (frame & 3) | ((frame >> 2) & 0x0C) | ((frame << 2) & 0x30); }

@@ -50,8 +50,8 @@ struct __attribute__((aligned(8))) Angle {
   float c, s;
 };
 
-// cos and sin of 2 pi x.  x = (quarter + r) / 4 with |r| <= 1/2; the Taylor polynomials' remainders at pi / 4 are 2e-9 (sine,
-// behind x^9) and 5e-11 (cosine, behind x^10).
+// cos and sin of 2 pi x.  x = (quarter + r) / 4 with |r| <= 1/2; the next terms of the Taylor series at pi / 4 are 2e-9 (sine,
+// behind x^9) and 1.2e-10 (cosine, behind x^10).
 __device__ __forceinline__ Angle angle_of(double turn) {
   const double q = rint(4.0 * turn);
   const float r = static_cast<float>(4.0 * turn - q) * 1.57079632679489662f;
