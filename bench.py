@@ -35,9 +35,10 @@ PEAK_BF16_TFLOPS = 2500.0    # dense bf16 MFMA
 # HBM traffic per launch in MiB (read, written) of each segment's kernels at the default
 # workload (65536 tokens), from rocprofv3 FETCH_SIZE / WRITE_SIZE scaled by a 1 GiB copy;
 # source: profiles/training_step_cfg5_hbm_traffic.txt.  Keys: (layer index, segment).
-# The figures belong to the kernels of library version PROFILED_VERSION; any other build
-# (a tile variant changed, a kernel rewritten) reports traffic as null instead of stale numbers.
-PROFILED_VERSION = 202
+# The figures belong to the kernels of the library versions PROFILED_VERSIONS (measured with 202; 203 added
+# entry points and left these kernels' code as it was, instruction for instruction); any other build (a
+# tile variant changed, a kernel rewritten) reports traffic as null instead of stale numbers.
+PROFILED_VERSIONS = (202, 203)
 MEASURED_TRAFFIC_MIB = {
     (0, "quantize_x"): (128.0 + 128.1, 0.1 + 32.0),      # abs-max pass + code pass
     (1, "quantize_x"): (512.0 + 512.1, 0.1 + 128.0),
@@ -408,7 +409,7 @@ def main():
 
     def seg_traffic(li, name):
         """Measured HBM bytes per launch (profiles/), or None away from the profiled workload."""
-        if args.tokens != 65536 or B.lib().aqt_version() != PROFILED_VERSION:
+        if args.tokens != 65536 or B.lib().aqt_version() not in PROFILED_VERSIONS:
             return None
         rd, wr = MEASURED_TRAFFIC_MIB[(li, name)]
         return (rd + wr) * 1048576.0

@@ -98,7 +98,7 @@ typedef struct aqt_saved {
 
 const char *aqt_status_string(aqt_status s); /* host, static storage */
 int aqt_last_hip_error(void);                /* hipError_t of this thread's last failed HIP call */
-int aqt_version(void);
+int aqt_version(void);                       /* 203: positions and the quantized cache joined */
 
 /* Bytes of workspace an op needs for the given shape (host computation, no GPU). 0 on bad args. */
 /* The backward ops' need does not fall as M grows: sized for the longest batch, it serves shorter ones. */
