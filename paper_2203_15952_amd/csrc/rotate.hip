@@ -201,14 +201,15 @@ struct Apart {
 // the instruction takes what lies under 2^-126 for zeros, or infinite) are scaled by a power of two first, v with them: by h h, and 1 / rms
 // is h h times the result.  A branch that the wavefront steps over where none of its heads is such.
 template <int L, int N>
-__device__ __forceinline__ float inverse_rms(float (&v)[N], float inv, float eps, float &h) {
+__device__ __forceinline__ float inverse_rms(float (&v)[N], float inv, float eps, bool value, float &h) {
   auto mean = [&] {
     float ss = 0.0f;
 #pragma unroll
     for (int i = 0; i < N; ++i) ss = fmaf(v[i], v[i], ss);
     return group_sum<L>(ss) * inv;
   };
-  float m = mean() + eps;
+  const float own = mean() + eps;   // (all lanes)
+  float m = value ? 1.0f : own;     // a value beside keys stays as it is
   h = 1.0f;
   if (__any(!(m >= 0x1p-100f && m < __builtin_inff()))) {
     h = m >= 0x1p-100f && m < __builtin_inff() ? 1.0f : m < 0x1p-100f ? 0x1p48f : 0x1p-48f;
@@ -222,7 +223,7 @@ __device__ __forceinline__ float inverse_rms(float (&v)[N], float inv, float eps
 // BWD: y is the upstream gradient, out the gradient with respect to x; GAINS: part [workgroups][2][dh] column sums (a kernel of its own,
 // for the registers of their sums: 32 x 400 rows of 1536 columns without them 33 us, and 36 in a kernel for both).
 template <class F, bool BWD, bool GAINS = BWD>
-__global__ __launch_bounds__(kThreads, GAINS ? 4 : 1) void rotate_kernel(const float *x, const float *y, RotateGeom g, float *out, float *part) {
+__global__ __launch_bounds__(kThreads, GAINS ? 4 : BWD ? 1 : 5) void rotate_kernel(const float *x, const float *y, RotateGeom g, float *out, float *part) {
   constexpr int L = F::LANES, N = F::N, GROUPS = 64 / L, U = BWD ? kBwdHeads : kFwdHeads, PAIRS = F::PAIRS;
   const int tid = static_cast<int>(threadIdx.x), lane = tid & 63, group = lane / L, j = lane % L;
   const F f(j, g.dh, g.rot);
@@ -253,7 +254,7 @@ __global__ __launch_bounds__(kThreads, GAINS ? 4 : 1) void rotate_kernel(const f
     for (int i = tid; i < kThreads / 64 * 2 * 128; i += kThreads) (&sums[0][0][0])[i] = 0.0;
   __syncthreads();
   // What the lanes have added up, over the groups of the wavefront, to its sums in float64.
-  auto hand_over = [&] {
+  auto hand_over = [&](auto in_between) {
 #pragma unroll
     for (int w = 0; w < 2; ++w)
 #pragma unroll
@@ -263,7 +264,7 @@ __global__ __launch_bounds__(kThreads, GAINS ? 4 : 1) void rotate_kernel(const f
         for (int off = L; off < 64; off <<= 1) s += __shfl_xor(s, off, 64);
         if (group == 0 && f.own(i)) sums[tid >> 6][w][f.column(i)] += static_cast<double>(s);
         dgain[w][i] = 0.0f;
-        __builtin_amdgcn_sched_barrier(0);   // one after the other: side by side they take registers from the rows
+        if (in_between()) __builtin_amdgcn_sched_barrier(0);   // one after the other: side by side they take registers from the rows
       }
   };
   int in_float = 0;
@@ -284,6 +285,13 @@ __global__ __launch_bounds__(kThreads, GAINS ? 4 : 1) void rotate_kernel(const f
     t = own - b * g.T;
   }
   for (int64_t m0 = begin; m0 < g.M; m0 += g.stride) {
+    if (GAINS) {
+      if (in_float >= kInFloat) {
+        in_float = 0;
+        hand_over([] { return true; });
+      }
+      in_float += steps;
+    }
     const int64_t m = m0 + row_of;
     const bool row_ok = m < g.M;
     const double frame = row_ok ? static_cast<double>((g.first ? g.first[b] : 0) + t) : 0.0;
@@ -320,13 +328,11 @@ __global__ __launch_bounds__(kThreads, GAINS ? 4 : 1) void rotate_kernel(const f
           for (int i = 0; i < N; ++i) u[i] = BWD ? w[k][i] : v[k][i];
         } else if (!BWD) {
           if (g.norm) {
-            float gain[N], x[N], half_scale;
+            float gain[N], half_scale;
             f.load_gains(gain, gains[query ? 0 : 1]);
+            const float r = inverse_rms<L>(v[k], inv, g.eps, value, half_scale);
 #pragma unroll
-            for (int i = 0; i < N; ++i) x[i] = v[k][i];
-            const float r = inverse_rms<L>(x, inv, g.eps, half_scale);
-#pragma unroll
-            for (int i = 0; i < N; ++i) u[i] = x[i] * r * gain[i];
+            for (int i = 0; i < N; ++i) u[i] = v[k][i] * r * gain[i];
           } else {
 #pragma unroll
             for (int i = 0; i < N; ++i) u[i] = v[k][i];
@@ -341,7 +347,7 @@ __global__ __launch_bounds__(kThreads, GAINS ? 4 : 1) void rotate_kernel(const f
           if (g.norm) {
             float gain[N], half_scale;
             f.load_gains(gain, gains[query ? 0 : 1]);
-            const float r = inverse_rms<L>(v[k], inv, g.eps, half_scale);
+            const float r = inverse_rms<L>(v[k], inv, g.eps, value, half_scale);
             float dot = 0.0f;
 #pragma unroll
             for (int i = 0; i < N; ++i) {
@@ -371,10 +377,6 @@ __global__ __launch_bounds__(kThreads, GAINS ? 4 : 1) void rotate_kernel(const f
         if (on) f.store(u, outr + static_cast<int64_t>(h) * g.dh);
       }
     }
-    if (GAINS && (in_float += steps) >= kInFloat) {
-      in_float = 0;
-      hand_over();
-    }
     b += g.stride_b;
     t += g.stride_t;
     if (t >= g.T) {
@@ -383,7 +385,7 @@ __global__ __launch_bounds__(kThreads, GAINS ? 4 : 1) void rotate_kernel(const f
     }
   }
   if constexpr (GAINS) {
-    hand_over();
+    hand_over([] { return false; });
     __syncthreads();
     if (tid < 2 * g.dh) {
       const int w = tid >= g.dh, c = w ? tid - g.dh : tid;
