@@ -11,7 +11,7 @@ struct CachedGeom {
   int64_t left, right;      // negative: no limit
   float scale_log2e;
 };
-// Wavefronts per SIMD that the kernel's registers are shared out to, without spills (dt: blocks of 16 head columns, r: rows).
+// Wavefronts per SIMD that the kernel's registers are shared out to, with five spilled at most (packed heads of 128: no slower so) (dt: blocks of 16 head columns, r: rows).
 constexpr int few_waves(int dt, bool packed, int r) { return dt == 8 ? (packed && r < 4 ? 3 : 2) : r > 1 && !packed ? 3 : 4; }
 constexpr int kFewRows = 4;   // rows per key / value head and stream up to which attention_cached_few.hip takes the call
 // part: the splits' rows, [rows][columns], then maxima and sums [rows] each, one after the other (nullptr: straight to ctx)

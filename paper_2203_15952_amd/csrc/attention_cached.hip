@@ -30,7 +30,7 @@ namespace {
 constexpr int kRows = 16;                 // rows of a workgroup
 // Wavefronts per SIMD that the kernel's registers are shared out to, without spills (dt: blocks of 16 head columns).
 constexpr int many_waves(int dt, bool packed) { return dt == 8 ? 2 : dt == 2 || packed ? 4 : 3; }
-// A row tile to a wavefront: fewer bytes of LDS (8192 row tiles of 128 int4 columns over 3 tiles: 95 us with two wavefronts, 90 so).
+// A row tile to a wavefront: fewer bytes of LDS, and three registers spilled for packed heads of 128 (8192 row tiles of 128 int4 columns over 3 tiles: 95 us with two wavefronts, 90 so).
 constexpr int own_waves(int dt, bool packed) { return dt == 8 && packed ? 3 : many_waves(dt, packed); }
 
 // The workgroup's place: (stream and head, row tile, split).  The row tiles of a split read the same codes; workgroup ids eight apart run
