@@ -714,10 +714,11 @@ aqt_status aqt_cache_advance(int64_t *length, int64_t streams, int64_t T, const 
  * before what the cache still holds) is zeros.  ctx_absmax nullable device float: max|ctx| over the
  * written rows, cleared by the call.  A non-finite query gives NaN in its row, a key or value kept as NaN
  * in the rows that see its frame; rows that do not see it come out as if it were not there.
- * Scores are as good as float32 sums (where one query column stands out, to 2^-46 of it; queries under 2^-100
- * lose bits).  The weights p_j s'_j (probability times the value's scale) are rounded to 2^-22 of the largest of
- * 64 frames, and no finer than 2^-123, and summed over those exactly: ctx is as good as float32 sums relative to
- * sum_j p_j max|v_j|, with the largest columns of the frames' values.
+ * Scores are as good as float32 sums, also where a few of a query's columns stand out from the others (one in heads
+ * of up to 8 columns; to 2^-46 of the largest; queries under 2^-100 lose bits).  The weights p_j s'_j (probability
+ * times the value's scale) are rounded to 2^-22 of the largest of 64 frames, and no finer than 2^-123, and summed
+ * over those exactly: ctx is as good as float32 sums relative to sum_j p_j max|v_j|, with the largest columns of the
+ * frames' values.
  * Needs aqt_attention_cached_workspace_bytes() (it does not depend on lengths or windows).
  */
 size_t aqt_attention_cached_workspace_bytes(const aqt_cache *cache, int64_t T, int heads);

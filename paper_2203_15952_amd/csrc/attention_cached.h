@@ -40,7 +40,7 @@ __device__ __forceinline__ void digits4(const int (&n)[4], int &d0, int &d1, int
 }
 
 // Whether a lane's 16 KS columns x of a row (from column 16 lg and 64 + 16 lg on, zeros behind dh) say that the row, whose largest column
-// is `top`, loses by integers relative to that: eight of them (twelve of 32, all others in narrow heads) lie under 1 / 64 of it.
+// is `top`, loses by integers relative to that: eight of them (twelve of 32; half of 9 to 15; all others of 8 and less) lie under 1 / 64 of it.
 // One in 25 of normally distributed columns does: it takes a row of 64 such columns once in three million (with six of them once in
 // ten thousand: one call in two of 8192 rows over a long history then waited for a row that it had taken, 62 us for 50).
 template <int KS>
@@ -53,7 +53,8 @@ __device__ __forceinline__ bool lane_is_wide(const float (&x)[KS][16], float top
 #pragma unroll
     for (int i = 0; i < 16; ++i) small += fabsf(x[k][i]) < below ? 1 : 0;
   }
-  return small >= min(max(dh - 1, 1), KS == 1 ? 8 : 12) && top < __builtin_inff();
+  const int enough = KS == 2 ? 12 : dh <= 8 ? max(dh - 1, 1) : min((dh + 1) / 2, 8);
+  return small >= enough && top < __builtin_inff();
 }
 // What a row's integers x `to` leave of it, in units of 2^-23 of theirs and again as digits (nothing of rows that are not wide: their
 // scores are the same with and without).

@@ -279,6 +279,8 @@ static void queries() {
   outlier_query(5, 3, 20, 4, 1e4f, 1);
   outlier_query(1, 1, 8, 8, 1e3f, 1);
   outlier_query(20, 1, 5, 8, 1e3f, 1);
+  outlier_query(2, 1, 9, 8, 1e3f, 3);
+  outlier_query(6, 1, 12, 4, 1e4f, 4);
   neighbours_of_outliers();
 }
 // Gains' gradients over many rows of a lane: the first of each a term of 1, the others 2^-25 and a little less, which a float32 sum
